@@ -54,9 +54,9 @@ enum {
   MONO_ERR_TIME = -2,   /* `now` decreased or is outside [0, MONO_MAX_NOW] */
   MONO_ERR_CUDA = -3,   /* a CUDA runtime call failed; see mono_last_cuda_error */
   MONO_ERR_NOMEM = -4,  /* device allocation failed, or the host memory a grouped call describes its tables in */
-  MONO_ERR_SIZE = -5,   /* caller buffer too small (mono_export) */
+  MONO_ERR_SIZE = -5,   /* caller buffer too small (mono_export, mono_token_rows_grad) */
   MONO_ERR_LIMIT = -6   /* the call is larger than the fixed maximum of an entry point that
-                           never allocates (mono_lookup_pool_noalloc) */
+                           never allocates (mono_lookup_pool_noalloc, mono_packed_scores) */
 };
 
 /* Sticky device-side condition bits reported in mono_status_t.error_bits. */
@@ -515,6 +515,106 @@ typedef struct {
 } mono_timing_t;
 int mono_timing_enable(mono_table* t, int on);
 int mono_timing_read(mono_table* t, mono_timing_t* host_out, int reset);
+
+/* ---- operators on plain matrices: fixed vocabularies, and rows in 4 bits ---- */
+
+/*
+ * A feature whose vocabulary is fixed and known (tokens of a sequence, categories, positions) needs no
+ * hash table: its rows are a matrix, and an ID is a row's number, here called a token.  The calls below
+ * are the pull and the push of such a matrix, one row per token instead of pooled bags, and the serving
+ * form of rows: 4 bits a column, looked up or scored against a vector.  mono_export and
+ * mono_read_rows write matrices that they take.  (The paper has no counterpart.)
+ *
+ * Conventions, besides those at the top:
+ *  - No table: the stream is an argument, the work runs on the current device, which has to be the one the
+ *    matrices are on, and nothing is allocated or kept, so calls can run at once on several streams (with a workspace each)
+ *    and be captured into CUDA graphs.  Descriptors are HOST structs, read before the call returns.
+ *  - A matrix that is written must not overlap anything else the call is given.
+ *  - Products and sums are taken in fp32, and what is written is rounded once, to nearest even.
+ *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS (a row of scores has one per packed row).
+ *  - A token outside [0, vocabulary) has no row: it looks up as zeros and its gradient is dropped, like MONO_RESERVED_ID in
+ *    a table.  So does the token `padding` (-1, or any other number outside the vocabulary, for none).
+ */
+#define MONO_MAX_COLS 65536
+
+enum { MONO_F32 = 0, MONO_BF16 = 1, MONO_F16 = 2 };   /* types of elements */
+enum { MONO_I32 = 0, MONO_I64 = 1 };                  /* types of tokens, signed */
+
+typedef struct {
+  void*   data;           /* DEVICE, aligned to its elements; may be NULL where rows is 0 */
+  int64_t rows, cols;
+  int64_t stride;         /* elements from a row to the next; >= cols where the matrix is written */
+  int32_t type;           /* MONO_F32, MONO_BF16 or MONO_F16 */
+  int32_t pad_;
+} mono_matrix_t;
+
+/*
+ * Rows by token:  out[i, :] = scale * weight[tokens[i], :], zeros where tokens[i] has no row.
+ *  weight   [vocabulary, cols]
+ *  tokens   DEVICE, n_tokens of token_type, aligned to their type
+ *  out      [n_tokens, cols], any of the types
+ */
+int mono_token_rows(const mono_matrix_t* weight, const void* tokens, int32_t token_type, int64_t n_tokens,
+                    int64_t padding, float scale, const mono_matrix_t* out, void* cuda_stream);
+
+/*
+ * Gradient of mono_token_rows:  G[v, :] = scale * sum of grad_out[i, :] over the i whose tokens[i] is v.
+ *  accumulate 0: grad_weight[v, :] = G[v, :] for every row v, zeros where no token is v;
+ *  accumulate 1: grad_weight[v, :] += G[v, :] for the rows that a token names (the sum rounded once), the other
+ *                rows are neither read nor written.
+ * The tokens are sorted (stably), and a row's terms are added up in an order that depends on the tokens alone: the same call on
+ * the same inputs gives the same bits.  (mono_apply_grads makes no such promise.)
+ *  grad_out     [n_tokens, cols]
+ *  grad_weight  [vocabulary, cols], any of the types
+ *  workspace    DEVICE, 256-byte aligned, workspace_bytes of it: at least what mono_token_rows_grad_workspace says for
+ *               these sizes (MONO_ERR_SIZE otherwise).  Needs no clearing and holds nothing afterwards; calls that may
+ *               run at once need one each, two captured graphs that are replayed at once as well.
+ */
+int mono_token_rows_grad(const mono_matrix_t* grad_out, const void* tokens, int32_t token_type, int64_t n_tokens,
+                         int64_t padding, float scale, int32_t accumulate, const mono_matrix_t* grad_weight,
+                         void* workspace, int64_t workspace_bytes, void* cuda_stream);
+/* bytes: HOST, receives the size */
+int mono_token_rows_grad_workspace(int64_t n_tokens, int64_t vocabulary, int64_t cols, int64_t* bytes);
+
+/*
+ * Rows in 4 bits.  Column c of row v stands for
+ *     (q(v, c) - 8) * scales[v, c / group],
+ * q(v, c) in 0 .. 15 being the low half of byte c / 2 of the row for an even c, the high half for an odd one.
+ */
+typedef struct {
+  uint8_t* q;             /* DEVICE [rows, q_stride], 16-byte aligned */
+  void*    scales;        /* DEVICE [rows, scale_stride], aligned to its elements */
+  int64_t  rows, cols;
+  int64_t  q_stride;      /* bytes from a row to the next: a multiple of 16, >= (cols + 1) / 2 rounded up to one */
+  int64_t  scale_stride;  /* elements from a row's scales to the next row's; >= the groups of a row */
+  int32_t  group;         /* 32, 64 or 128 columns; the last group of a row may have fewer */
+  int32_t  scale_type;    /* MONO_F32, MONO_BF16 or MONO_F16 */
+} mono_packed_t;
+
+/*
+ * Packs rows: of each group, scale = (largest |column|) / 7 rounded to scale_type, and
+ * q = 8 + (column / scale rounded to nearest even, held within -7 .. 7), 8 where the scale is 0.  A group with a column
+ * that is not finite gets a scale that is not finite and q = 8: all of its values are NaN (as are those of a group whose scale is
+ * beyond scale_type).  Halves of bytes behind the last column, up to (cols + 1) / 2 bytes rounded up to a multiple of 16, are 8.
+ */
+int mono_pack_rows(const mono_matrix_t* rows, const mono_packed_t* packed, void* cuda_stream);
+
+/* mono_token_rows of packed rows:  out[i, c] = scale * value(tokens[i], c). */
+int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int32_t token_type, int64_t n_tokens,
+                           int64_t padding, float scale, const mono_matrix_t* out, void* cuda_stream);
+
+/*
+ * Scores of every packed row against a few vectors (a user's vector against all candidates; the output layer that shares
+ * the input layer's matrix):  out[m, v] = sum over c of x[m, c] * value(v, c), taken as
+ *     sum over groups of  scale(v, group) * (sum over the group's c of x[m, c] * (q(v, c) - 8)),
+ * each in fp32, no product rounded to fewer bits.
+ *  x        [up to MONO_MAX_SCORED, packed->cols]; MONO_ERR_LIMIT for more rows: that is a matrix product
+ *  out      [x->rows, packed->rows], any of the types
+ * MONO_ERR_LIMIT too for more than MONO_MAX_SCORED_COLS columns.
+ */
+#define MONO_MAX_SCORED 16
+#define MONO_MAX_SCORED_COLS 8192
+int mono_packed_scores(const mono_packed_t* packed, const mono_matrix_t* x, const mono_matrix_t* out, void* cuda_stream);
 
 /* Text of the last CUDA error seen by this table (HOST string, library-owned). */
 const char* mono_last_cuda_error(mono_table* t);

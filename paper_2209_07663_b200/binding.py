@@ -27,6 +27,9 @@ MONO_OK, MONO_ERR_ARG, MONO_ERR_TIME, MONO_ERR_CUDA, MONO_ERR_NOMEM, MONO_ERR_SI
 MONO_ERR_LIMIT = -6
 MONO_NOALLOC_MAX_IDS = 1 << 20
 MONO_DEV_ROWS_FULL, MONO_DEV_KEYS_FULL, MONO_DEV_BAD_OFFSETS, MONO_DEV_IMPORT_DUP, MONO_DEV_INTERNAL = 1, 2, 4, 8, 16
+MONO_F32, MONO_BF16, MONO_F16 = 0, 1, 2
+MONO_I32, MONO_I64 = 0, 1
+MONO_MAX_COLS, MONO_MAX_SCORED, MONO_MAX_SCORED_COLS = 65536, 16, 8192
 MONO_RESERVED_ID = 0xFFFFFFFFFFFFFFFF
 MONO_MAX_NOW = 0xFFFFFFFE
 
@@ -36,7 +39,8 @@ EXPORTS = [
     "mono_probe", "mono_read_rows", "mono_export", "mono_import", "mono_audit", "mono_last_cuda_error",
     "mono_error_string", "mono_timing_enable", "mono_timing_read", "mono_lookup_pool_noalloc", "mono_export_touched", "mono_rehash", "mono_expire_slice", "mono_prepare_push", "mono_group_ahead",
     "mono_group_lookup_pool", "mono_group_apply_grads", "mono_group_prepare_push", "mono_fence", "mono_snapshot_save", "mono_snapshot_restore",
-    "mono_snapshot_drop",
+    "mono_snapshot_drop", "mono_token_rows", "mono_token_rows_grad", "mono_token_rows_grad_workspace", "mono_pack_rows",
+    "mono_packed_token_rows", "mono_packed_scores",
 ]
 
 
@@ -81,6 +85,17 @@ class mono_timing_t(ctypes.Structure):
                 ("kernel", mono_kernel_time_t * 24)]
 
 
+class mono_matrix_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("pad_", ctypes.c_int32)]
+
+
+class mono_packed_t(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64), ("group", ctypes.c_int32),
+                ("scale_type", ctypes.c_int32)]
+
+
 def _struct_dict(s: ctypes.Structure) -> dict:
     return {name: getattr(s, name) for name, _ in s._fields_ if not name.startswith("pad")}
 
@@ -101,6 +116,7 @@ def load_library(path: Optional[str] = None):
                            "(there is no non-CUDA fallback)")
     L = ctypes.CDLL(path)
     vp, i64, u64, u32, ci = ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int
+    i32, f32, matrix, packed = ctypes.c_int32, ctypes.c_float, ctypes.POINTER(mono_matrix_t), ctypes.POINTER(mono_packed_t)
     proto = {
         "mono_table_create": (ci, [ctypes.POINTER(vp), u64, u32, u32, u32, ctypes.POINTER(mono_opt), vp]),
         "mono_table_destroy": (ci, [vp]),
@@ -132,6 +148,12 @@ def load_library(path: Optional[str] = None):
         "mono_snapshot_save": (ci, [vp]),
         "mono_snapshot_restore": (ci, [vp]),
         "mono_snapshot_drop": (ci, [vp]),
+        "mono_token_rows": (ci, [matrix, vp, i32, i64, i64, f32, matrix, vp]),
+        "mono_token_rows_grad": (ci, [matrix, vp, i32, i64, i64, f32, i32, matrix, vp, i64, vp]),
+        "mono_token_rows_grad_workspace": (ci, [i64, i64, i64, ctypes.POINTER(i64)]),
+        "mono_pack_rows": (ci, [matrix, packed, vp]),
+        "mono_packed_token_rows": (ci, [packed, vp, i32, i64, i64, f32, matrix, vp]),
+        "mono_packed_scores": (ci, [packed, matrix, matrix, vp]),
         "mono_timing_enable": (ci, [vp, ci]),
         "mono_timing_read": (ci, [vp, ctypes.POINTER(mono_timing_t), ci]),
     }
@@ -164,6 +186,11 @@ class _Portable:
             fn = getattr(L, "mono_" + name)
             setattr(self, name, lambda *args, fn=fn: fn(*map(_ptr, args)))
         self._lib = L
+
+    def _tensors_only(self, *args):
+        raise TypeError("torch tensors are expected")
+
+    token_rows = token_rows_grad = pack_rows = packed_token_rows = packed_scores = _tensors_only
 
     @staticmethod
     def _group(handles, ids, slot_offsets, vectors):
@@ -413,6 +440,52 @@ def mono_timing_read(t: int, reset: bool = False) -> dict:
     ks = {tm.kernel[i].name.decode(): {"launches": int(tm.kernel[i].launches), "ms": float(tm.kernel[i].ms)}
           for i in range(tm.n_kernels)}
     return {"launches_total": int(tm.launches_total), "kernels": ks}
+
+
+# ---- operators on plain matrices: torch tensors on one CUDA device, whose current stream the work runs on ----
+# (a program without torch describes its matrices with mono_matrix_t and mono_packed_t and calls load_library()'s functions)
+
+def mono_token_rows(weight, tokens, out, *, scale: float = 1.0, padding: int = -1) -> None:
+    """out[i] = scale * weight[tokens[i]]; zeros where the token is `padding` or outside the vocabulary."""
+    rc = (_native or _hot()).token_rows(weight, tokens, out, scale, padding)
+    if rc:
+        _check("mono_token_rows", rc)
+
+
+def mono_token_rows_grad(grad_out, tokens, grad_weight, *, scale: float = 1.0, padding: int = -1, accumulate: bool = False,
+                         workspace=None) -> None:
+    """grad_weight[v] = scale * the sum of grad_out[i] over the tokens i that are v (accumulate: added to the rows that tokens
+    name).  workspace: mono_token_rows_grad_workspace() bytes on the device; None takes them from torch's allocator."""
+    rc = (_native or _hot()).token_rows_grad(grad_out, tokens, grad_weight, scale, padding, accumulate, workspace)
+    if rc:
+        _check("mono_token_rows_grad", rc)
+
+
+def mono_token_rows_grad_workspace(n_tokens: int, vocabulary: int, cols: int) -> int:
+    n = ctypes.c_int64(0)
+    _check("mono_token_rows_grad_workspace", load_library().mono_token_rows_grad_workspace(n_tokens, vocabulary, cols, ctypes.byref(n)))
+    return n.value
+
+
+def mono_pack_rows(rows, q, scales, group: int) -> None:
+    """Rows in 4 bits: q uint8 [rows, bytes], scales [rows, groups]; see PackedRows."""
+    rc = (_native or _hot()).pack_rows(rows, q, scales, group)
+    if rc:
+        _check("mono_pack_rows", rc)
+
+
+def mono_packed_token_rows(q, scales, group: int, tokens, out, *, scale: float = 1.0, padding: int = -1) -> None:
+    """mono_token_rows of packed rows (as many columns as `out` has)."""
+    rc = (_native or _hot()).packed_token_rows(q, scales, group, tokens, out, scale, padding)
+    if rc:
+        _check("mono_packed_token_rows", rc)
+
+
+def mono_packed_scores(q, scales, group: int, x, out) -> None:
+    """out[m, v] = <x[m], row v> for every packed row v and up to MONO_MAX_SCORED vectors."""
+    rc = (_native or _hot()).packed_scores(q, scales, group, x, out)
+    if rc:
+        _check("mono_packed_scores", rc)
 
 
 # ---- a small convenience wrapper over torch tensors -------------------------

@@ -11,6 +11,7 @@ import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
+HEADER = os.path.join(PKG, "..", "include", "mono.h")
 LIB = os.path.join(PKG, "libmono.so")
 # the same sources with -DMONO_DEBUG: every index the library computes for itself is range-checked
 # on the device and a bad one reported through the status bits (binding: MONO_LIBRARY=checked)
@@ -19,7 +20,7 @@ LIB_CHECKED = os.path.join(PKG, "libmono_checked.so")
 NATIVE_SOURCE = os.path.join(CSRC, "binding_native.cpp")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "--cudart", "static", "-ldl"]
+              "-shared", "-Xcompiler", "-fPIC", "--cudart", "static", "-ldl", "--threads", "4"]
 
 
 def _sources():
@@ -27,7 +28,7 @@ def _sources():
 
 
 def _newest_input() -> float:
-    files = glob.glob(os.path.join(CSRC, "*.cu*")) + [os.path.join(PKG, "..", "include", "mono.h")]
+    files = glob.glob(os.path.join(CSRC, "*.cu*")) + [HEADER]
     return max(os.path.getmtime(f) for f in files)
 
 
@@ -49,7 +50,7 @@ def native_path() -> str:
 def build_native(force: bool = False) -> str:
     """Compile csrc/binding_native.cpp against the torch that is installed, unless it is up to date."""
     native = native_path()
-    if not force and os.path.exists(native) and os.path.getmtime(native) >= os.path.getmtime(NATIVE_SOURCE):
+    if not force and os.path.exists(native) and os.path.getmtime(native) >= max(map(os.path.getmtime, (NATIVE_SOURCE, HEADER))):
         return native
     import torch
     from torch.utils import cpp_extension
@@ -58,7 +59,8 @@ def build_native(force: bool = False) -> str:
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            *[f"-isystem{d}" for d in cpp_extension.include_paths()], f"-I{sysconfig.get_paths()['include']}",
-           NATIVE_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"]
+           f"-isystem{os.path.join(os.path.dirname(os.path.dirname(find_nvcc())), 'include')}",
+           NATIVE_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
     subprocess.check_call(cmd)
     os.replace(tmp, native)
     return native

@@ -3,8 +3,8 @@
 // binding.py declares every call; the ones a training or serving loop makes each step come here.
 // What bounds a small batch is the host: through ctypes a call with three tensors cost 2.6 us before
 // it reached the library (two Python method calls per tensor, argument conversion), a grouped call
-// over 64 tables 85 us.  Here a tensor is unpacked in a few nanoseconds.  No work of the table is
-// done in this file.
+// over 64 tables 85 us.  Here a tensor is unpacked in a few nanoseconds.  No work of the table or of
+// an operator is done in this file.
 #include <Python.h>
 
 #include <cstdint>
@@ -13,7 +13,12 @@
 #include <vector>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include "../../include/mono.h"
 
 namespace {
 
@@ -24,12 +29,14 @@ using ptr = void*;
 // Addresses of the library's functions, set once by bind().
 enum Fn {
   F_LOOKUP, F_LOOKUP_NOALLOC, F_LOOKUP_HOST, F_APPLY, F_APPLY_HOST, F_PREPARE, F_AHEAD, F_EXPIRE, F_EXPIRE_SLICE, F_FENCE,
-  F_GROUP_PREPARE, F_GROUP_LOOKUP, F_GROUP_APPLY, F_COUNT
+  F_GROUP_PREPARE, F_GROUP_LOOKUP, F_GROUP_APPLY, F_TOKEN_ROWS, F_TOKEN_ROWS_GRAD, F_TOKEN_ROWS_GRAD_WORKSPACE, F_PACK_ROWS,
+  F_PACKED_TOKEN_ROWS, F_PACKED_SCORES, F_COUNT
 };
 const char* const kNames[F_COUNT] = {
   "mono_lookup_pool", "mono_lookup_pool_noalloc", "mono_lookup_pool_host", "mono_apply_grads", "mono_apply_grads_host",
   "mono_prepare_push", "mono_group_ahead", "mono_expire", "mono_expire_slice", "mono_fence", "mono_group_prepare_push",
-  "mono_group_lookup_pool", "mono_group_apply_grads"
+  "mono_group_lookup_pool", "mono_group_apply_grads", "mono_token_rows", "mono_token_rows_grad", "mono_token_rows_grad_workspace", "mono_pack_rows",
+  "mono_packed_token_rows", "mono_packed_scores"
 };
 ptr g_fn[F_COUNT] = {};
 PyObject* g_address_of = nullptr;      // binding._ptr, for what is neither a tensor, an int nor None
@@ -266,6 +273,187 @@ PyObject* group_push(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- operators on plain matrices: tensors as they are, on the current stream of their device ----
+
+// The tensors of one call, in turn.  All of them have to be on one CUDA device; it is the current one while the call
+// runs, and an output's version goes up, so that autograd sees that it was written.
+struct Operands {
+  const at::Device* device = nullptr;
+
+  const at::Tensor* tensor(PyObject* x, const char* name) {
+    if (!THPVariable_CheckExact(x)) { PyErr_Format(PyExc_TypeError, "%s: a torch.Tensor is expected, not %s", name, Py_TYPE(x)->tp_name); return nullptr; }
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (!t.is_cuda()) { PyErr_Format(PyExc_ValueError, "%s is not on a CUDA device (there is no CPU path)", name); return nullptr; }
+    if (!device) { at_ = t.device(); device = &at_; }
+    if (t.device() != at_) { PyErr_Format(PyExc_ValueError, "%s is on another device than the tensors before it", name); return nullptr; }
+    return &t;
+  }
+
+  // Rows of elements next to each other: a 2-d tensor with any distance between its rows, or a contiguous one of any shape.
+  bool matrix(PyObject* x, const char* name, bool written, mono_matrix_t* m) {
+    const at::Tensor* t = tensor(x, name);
+    if (!t) return false;
+    switch (t->scalar_type()) {
+      case at::kFloat: m->type = MONO_F32; break;
+      case at::kBFloat16: m->type = MONO_BF16; break;
+      case at::kHalf: m->type = MONO_F16; break;
+      default: PyErr_Format(PyExc_TypeError, "%s: float32, bfloat16 or float16 is expected", name); return false;
+    }
+    const i64 dims = t->dim();
+    if (dims < 1) { PyErr_Format(PyExc_ValueError, "%s is a single number, not rows", name); return false; }
+    m->cols = t->size(dims - 1);
+    if (dims == 2 && (m->cols <= 1 || t->stride(1) == 1)) {
+      m->rows = t->size(0);
+      m->stride = m->rows > 1 ? t->stride(0) : m->cols;
+    } else if (t->is_contiguous()) {
+      m->rows = m->cols ? t->numel() / m->cols : 0;
+      m->stride = m->cols;
+    } else {
+      PyErr_Format(PyExc_ValueError, "%s: the columns of a row have to be next to each other", name);
+      return false;
+    }
+    m->data = t->data_ptr();
+    m->pad_ = 0;
+    if (written && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+    return true;
+  }
+
+  bool tokens(PyObject* x, const void** data, int32_t* type, i64* n) {
+    const at::Tensor* t = tensor(x, "tokens");
+    if (!t) return false;
+    if (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong) { PyErr_SetString(PyExc_TypeError, "tokens: int32 or int64 is expected"); return false; }
+    if (!t->is_contiguous()) { PyErr_SetString(PyExc_ValueError, "tokens have to be contiguous"); return false; }
+    *type = t->scalar_type() == at::kInt ? MONO_I32 : MONO_I64;
+    *data = t->data_ptr();
+    *n = t->numel();
+    return true;
+  }
+
+  // q and scales of rows that have `cols` columns
+  bool packed(PyObject* q, PyObject* scales, PyObject* group, i64 cols, mono_packed_t* p) {
+    i64 g;
+    if (!integer(group, &g)) return false;
+    if (g != 32 && g != 64 && g != 128) { PyErr_SetString(PyExc_ValueError, "group: 32, 64 or 128 is expected"); return false; }
+    const at::Tensor* t = tensor(q, "q");
+    mono_matrix_t s;
+    if (!t || !matrix(scales, "scales", false, &s)) return false;
+    const i64 bytes = (cols + 31) / 32 * 16, groups = (cols + g - 1) / g;
+    if (t->scalar_type() != at::kByte) { PyErr_SetString(PyExc_TypeError, "q: uint8 is expected"); return false; }
+    if (t->dim() != 2 || t->size(1) < bytes || t->stride(1) != 1) {
+      PyErr_Format(PyExc_ValueError, "q: rows of at least %lld bytes next to each other are expected", (long long)bytes);
+      return false;
+    }
+    if (s.rows != t->size(0) || s.cols < groups) {
+      PyErr_Format(PyExc_ValueError, "scales: a row of at least %lld scales is expected for each row of q", (long long)groups);
+      return false;
+    }
+    p->q = static_cast<uint8_t*>(t->data_ptr());
+    p->scales = s.data;
+    p->rows = t->size(0);
+    p->cols = cols;
+    p->q_stride = p->rows > 1 ? t->stride(0) : bytes;
+    p->scale_stride = p->rows > 1 ? s.stride : groups;
+    p->group = (int32_t)g;
+    p->scale_type = s.type;
+    return true;
+  }
+
+  template <typename C>
+  PyObject* run(C&& call) {
+    const c10::DeviceGuard guard(at_);
+    const ptr stream = c10::cuda::getCurrentCUDAStream(at_.index()).stream();
+    return without_gil([&] { return call(stream); });
+  }
+
+ private:
+  at::Device at_ = at::kCPU;
+};
+
+bool number(PyObject* x, float* out) {
+  *out = (float)PyFloat_AsDouble(x);
+  return !PyErr_Occurred();
+}
+
+// (weight, tokens, out, scale, padding)
+PyObject* token_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Operands o;
+  mono_matrix_t weight, out;
+  const void* tokens;
+  int32_t type;
+  i64 count, padding;
+  float scale;
+  if (!expects(n, 5) || !number(a[3], &scale) || !integer(a[4], &padding) || !o.matrix(a[0], "weight", false, &weight) ||
+      !o.tokens(a[1], &tokens, &type, &count) || !o.matrix(a[2], "out", true, &out)) return nullptr;
+  return o.run([&](ptr s) { return fn<decltype(&mono_token_rows)>(F_TOKEN_ROWS)(&weight, tokens, type, count, padding, scale, &out, s); });
+}
+
+// (grad_out, tokens, grad_weight, scale, padding, accumulate, workspace or None)
+PyObject* token_rows_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Operands o;
+  mono_matrix_t grad, out;
+  const void* tokens;
+  int32_t type;
+  i64 count, padding, bytes = 0;
+  float scale;
+  if (!expects(n, 7) || !number(a[3], &scale) || !integer(a[4], &padding)) return nullptr;
+  const int accumulate = PyObject_IsTrue(a[5]);
+  if (accumulate < 0 || !o.matrix(a[0], "grad_out", false, &grad) || !o.tokens(a[1], &tokens, &type, &count) || !o.matrix(a[2], "grad_weight", true, &out)) return nullptr;
+  at::Tensor made;
+  ptr workspace;
+  if (a[6] == Py_None) {
+    const int rc = fn<decltype(&mono_token_rows_grad_workspace)>(F_TOKEN_ROWS_GRAD_WORKSPACE)(count, out.rows, out.cols, &bytes);
+    if (rc) return PyLong_FromLong(rc);
+    const c10::DeviceGuard guard(*o.device);
+    made = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(*o.device));
+    workspace = made.data_ptr();
+  } else {
+    const at::Tensor* t = o.tensor(a[6], "workspace");
+    if (!t) return nullptr;
+    if (!t->is_contiguous()) { PyErr_SetString(PyExc_ValueError, "workspace has to be contiguous"); return nullptr; }
+    workspace = t->data_ptr();
+    bytes = (i64)t->nbytes();
+  }
+  return o.run([&](ptr s) {
+    return fn<decltype(&mono_token_rows_grad)>(F_TOKEN_ROWS_GRAD)(&grad, tokens, type, count, padding, scale, accumulate, &out, workspace, bytes, s);
+  });
+}
+
+// (rows, q, scales, group)
+PyObject* pack_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Operands o;
+  mono_matrix_t rows;
+  mono_packed_t packed;
+  if (!expects(n, 4) || !o.matrix(a[0], "rows", false, &rows) || !o.packed(a[1], a[2], a[3], rows.cols, &packed)) return nullptr;
+  for (PyObject* x : {a[1], a[2]}) {
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
+  return o.run([&](ptr s) { return fn<decltype(&mono_pack_rows)>(F_PACK_ROWS)(&rows, &packed, s); });
+}
+
+// (q, scales, group, tokens, out, scale, padding)
+PyObject* packed_token_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Operands o;
+  mono_matrix_t out;
+  mono_packed_t packed;
+  const void* tokens;
+  int32_t type;
+  i64 count, padding;
+  float scale;
+  if (!expects(n, 7) || !number(a[5], &scale) || !integer(a[6], &padding) || !o.matrix(a[4], "out", true, &out) || !o.packed(a[0], a[1], a[2], out.cols, &packed) ||
+      !o.tokens(a[3], &tokens, &type, &count)) return nullptr;
+  return o.run([&](ptr s) { return fn<decltype(&mono_packed_token_rows)>(F_PACKED_TOKEN_ROWS)(&packed, tokens, type, count, padding, scale, &out, s); });
+}
+
+// (q, scales, group, x, out)
+PyObject* packed_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Operands o;
+  mono_matrix_t x, out;
+  mono_packed_t packed;
+  if (!expects(n, 5) || !o.matrix(a[3], "x", false, &x) || !o.matrix(a[4], "out", true, &out) || !o.packed(a[0], a[1], a[2], x.cols, &packed)) return nullptr;
+  return o.run([&](ptr s) { return fn<decltype(&mono_packed_scores)>(F_PACKED_SCORES)(&packed, &x, &out, s); });
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(static_cast<Method>(guarded<f>))), METH_FASTCALL, nullptr
 PyMethodDef kMethods[] = {
   {"bind", FAST(bind)},
@@ -283,6 +471,11 @@ PyMethodDef kMethods[] = {
   {"group_prepare_push", FAST(group_prepare)},
   {"group_lookup_pool", FAST(group_pull)},
   {"group_apply_grads", FAST(group_push)},
+  {"token_rows", FAST(token_rows)},
+  {"token_rows_grad", FAST(token_rows_grad)},
+  {"pack_rows", FAST(pack_rows)},
+  {"packed_token_rows", FAST(packed_token_rows)},
+  {"packed_scores", FAST(packed_scores)},
   {nullptr, nullptr, 0, nullptr}
 };
 

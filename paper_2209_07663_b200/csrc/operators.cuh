@@ -1,0 +1,110 @@
+// What the operators on plain matrices (token_rows.cu, packed_rows.cu) share: the element types, checked
+// views of the caller's matrices, vectors of elements, and launches.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+#include <utility>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <nvtx3/nvToolsExt.h>
+
+#include "../../include/mono.h"
+
+namespace mono {
+
+// profiler range of one call, named after the entry point
+struct OperatorRange {
+  explicit OperatorRange(const char* name) { nvtxRangePushA(name); }
+  ~OperatorRange() { nvtxRangePop(); }
+};
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+// (to nearest, ties to even: an output is rounded once, here)
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// N consecutive elements, moved in accesses of up to 16 bytes
+template <typename T, int N>
+struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Vec { T v[N]; };
+
+constexpr uint32_t kNoToken = 0xFFFFFFFFu;
+constexpr int64_t kMaxOperatorRows = 0x7FFFFFFEll;      // of a matrix, and tokens of a call
+
+// The caller's tokens: 32 or 64 bits, signed.
+struct TokenList {
+  const void* data;
+  int64_t n;
+  int64_t vocab;
+  int64_t padding;
+  bool wide;
+  // the row that token i names, or kNoToken: outside the vocabulary, or the padding
+  __device__ __forceinline__ uint32_t at(int64_t i) const {
+    const int64_t t = wide ? static_cast<const int64_t*>(data)[i] : static_cast<const int32_t*>(data)[i];
+    return (uint64_t)t < (uint64_t)vocab && t != padding ? (uint32_t)t : kNoToken;
+  }
+};
+
+inline int element_size(int32_t type) { return type == MONO_F32 ? 4 : type == MONO_BF16 || type == MONO_F16 ? 2 : 0; }
+inline bool is_aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Whether m describes a matrix that can be read, or written (then no two of its rows may overlap).
+inline bool matrix_ok(const mono_matrix_t* m, bool written) {
+  if (!m) return false;
+  const int size = element_size(m->type);
+  if (!size || m->rows < 0 || m->rows > kMaxOperatorRows || m->cols < 1 || m->cols > MONO_MAX_COLS) return false;
+  if (m->rows == 0) return true;
+  if (m->stride < 0 || m->stride > (int64_t)1 << 40 || (written && m->rows > 1 && m->stride < m->cols)) return false;
+  return m->data && is_aligned(m->data, size);
+}
+
+inline bool tokens_ok(const void* tokens, int32_t type, int64_t n) {
+  const int size = type == MONO_I32 ? 4 : type == MONO_I64 ? 8 : 0;
+  return size && n >= 0 && n <= kMaxOperatorRows && (n == 0 || (tokens && is_aligned(tokens, size)));
+}
+
+// The most elements (8, 4, 2 or 1) that can be moved at once at every multiple of as many columns of every row.
+inline int vector_of(const mono_matrix_t& m) {
+  const int size = element_size(m.type);
+  for (int v = 8; v > 1; v /= 2) {
+    const size_t bytes = std::min(16, v * size);
+    if (m.cols % v == 0 && is_aligned(m.data, bytes) && (m.rows <= 1 || m.stride * size % (int64_t)bytes == 0)) return v;
+  }
+  return 1;
+}
+
+// Calls f with a value of the element type / of the vector's width.
+template <typename F>
+int with_type(int32_t type, F&& f) {
+  return type == MONO_F32 ? f(float()) : type == MONO_BF16 ? f(__nv_bfloat16()) : f(__half());
+}
+template <int N> struct Width { static constexpr int value = N; };
+template <typename F>
+int with_width(int v, F&& f) {
+  return v == 8 ? f(Width<8>()) : v == 4 ? f(Width<4>()) : v == 2 ? f(Width<2>()) : f(Width<1>());
+}
+
+// Launch of a kernel that waits for the stream's previous kernel itself (after_previous_kernel), so that its
+// launch is prepared while that one runs.
+template <typename... P, typename... A>
+inline int launch_operator(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, cudaStream_t s, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block, 1, 1);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess ? MONO_OK : MONO_ERR_CUDA;
+}
+
+}  // namespace mono

@@ -1,0 +1,404 @@
+// Rows in 4 bits (mono_pack_rows, mono_packed_token_rows, mono_packed_scores): kernels and host side.
+#include <climits>
+
+#include "operators.cuh"
+#include "table_layout.cuh"
+
+using namespace mono;
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct PackedView {
+  uint8_t* q;
+  void* scales;
+  int64_t rows, q_stride, scale_stride;
+  int cols, groups;
+};
+
+inline bool packed_ok(const mono_packed_t* p) {
+  if (!p || !element_size(p->scale_type) || (p->group != 32 && p->group != 64 && p->group != 128)) return false;
+  if (p->rows < 0 || p->rows > kMaxOperatorRows || p->cols < 1 || p->cols > MONO_MAX_COLS) return false;
+  if (p->rows == 0) return true;
+  if (p->q_stride % 16 || p->q_stride < (p->cols + 31) / 32 * 16 || p->q_stride > (int64_t)1 << 40) return false;
+  if (p->scale_stride < (p->cols + p->group - 1) / p->group || p->scale_stride > (int64_t)1 << 40) return false;
+  return p->q && is_aligned(p->q, 16) && p->scales && is_aligned(p->scales, element_size(p->scale_type));
+}
+
+inline PackedView view(const mono_packed_t& p) {
+  return {p.q, p.scales, p.rows, p.q_stride, p.scale_stride, (int)p.cols, (int)((p.cols + p.group - 1) / p.group)};
+}
+
+// ---------------------------------------------------------------------------
+// Packing: 16 threads a group of columns, group / 16 neighbouring columns each, so that every thread writes whole bytes.
+// ---------------------------------------------------------------------------
+template <typename W, typename S, int GROUP>
+__global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* __restrict__ rows, int64_t stride, PackedView p) {
+  after_previous_kernel();
+  constexpr int N = GROUP / 16;
+  const int lane = threadIdx.x % 16;
+  const int64_t item = (int64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16;
+  const int64_t row = item / p.groups;
+  if (row >= p.rows) return;                                // (all 16 threads of a group)
+  const unsigned members = 0xFFFFu << (threadIdx.x & 16);
+  const int g = (int)(item % p.groups), c0 = g * GROUP + lane * N;
+  float w[N];
+  float most = 0.0f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    w[i] = c0 + i < p.cols ? to_float(rows[row * stride + c0 + i]) : 0.0f;
+    most = fmaxf(most, fabsf(w[i]));                        // (fmaxf passes over a NaN)
+    nan |= w[i] != w[i];
+  }
+#pragma unroll
+  for (int s = 8; s > 0; s /= 2) {
+    most = fmaxf(most, __shfl_xor_sync(members, most, s));
+    nan |= __shfl_xor_sync(members, (int)nan, s) != 0;
+  }
+  const S stored = from_float<S>(nan ? __int_as_float(0x7FC00000) : __fdiv_rn(most, 7.0f));
+  const float scale = to_float(stored);
+  const bool usable = scale > 0.0f && scale <= 3.402823466e38f;
+  const int64_t padded = (int64_t)((p.cols + 31) / 32) * 16;      // bytes of a row that are written
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    int q[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float r = usable ? fminf(fmaxf(rintf(__fdiv_rn(w[i + j], scale)), -7.0f), 7.0f) : 0.0f;
+      q[j] = (int)r + 8;
+    }
+    const int64_t byte = (c0 + i) / 2;
+    if (byte < padded) p.q[row * p.q_stride + byte] = (uint8_t)(q[0] | q[1] << 4);
+  }
+  if (lane == 0) static_cast<S*>(p.scales)[row * p.scale_stride + g] = stored;
+}
+
+// ---------------------------------------------------------------------------
+// Rows by token of packed rows: a thread makes the 8 columns of one 32-bit word.
+// ---------------------------------------------------------------------------
+template <typename S, typename O, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView p, int group_words, TokenList tokens, float scale, O* __restrict__ out, int64_t out_stride, int lanes) {
+  after_previous_kernel();
+  const int lane = threadIdx.x & (lanes - 1);
+  const int64_t i = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
+  if (i >= tokens.n) return;
+  const uint32_t t = tokens.at(i);
+  const int words = (p.cols + 7) / 8;
+  for (int w = blockIdx.y * lanes + lane; w < words; w += gridDim.y * lanes) {
+    uint32_t q = 0;
+    float s = 0.0f;
+    if (t != kNoToken) {
+      q = *reinterpret_cast<const uint32_t*>(p.q + t * p.q_stride + (int64_t)w * 4);
+      s = to_float(static_cast<const S*>(p.scales)[t * p.scale_stride + w / group_words]);
+    }
+    Vec<O, 8> o;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o.v[c] = from_float<O>(t != kNoToken ? scale * ((float)((int)(q >> (4 * c) & 15) - 8) * s) : 0.0f);
+    O* at = out + i * out_stride + (int64_t)w * 8;
+    if (ALIGNED) {
+      *reinterpret_cast<Vec<O, 8>*>(at) = o;
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (w * 8 + c < p.cols) at[c] = o.v[c];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Scores.  out[m, v] = sum over groups g of s[v, g] * (sum over c in g of x[m, c] * (q[v, c] - 8)).
+//
+// The bytes of q bound it (half a byte for 2 * m operations), so a weight has to become an operand in few instructions: the tensor
+// cores' 16-bit products take 16 rows and 8 vectors at once.  4 bits placed in the low mantissa of 2^7 (bf16) or 2^10 (fp16)
+// are 128 + q or 1024 + q; less 136 or 1032, exact in either type, they are q - 8: with the shift, one and a half instructions
+// per two weights.  Vectors in fp32 are three bf16 vectors whose sum they are exactly (8 bits of the significand each).  All products are exact, all sums in fp32.
+//
+// In a product of mma.m16n8k16 the columns are summed over, so any may stand in any place, as long as the vectors' are in the same.
+// So the rows are read as they lie: of a group of columns, thread t of the four that share a row has the t-th quarter of its
+// bytes, in one load (4, 8 or 16 bytes), and what the masks select of a word, columns p and p + 4, is a pair for the product.  The vectors are laid
+// out in shared memory to match, once per block.
+//
+// A warp has 16 rows at a time; where rows are long, `split` warps share 16 rows, a run of groups each.
+// ---------------------------------------------------------------------------
+constexpr int kTileRows = 16;
+
+struct Bf16Operand {
+  using T = __nv_bfloat16;
+  static __device__ __forceinline__ uint32_t pair(uint32_t w) {            // columns in bits 0..3 and 16..19
+    const uint32_t biased = (w & 0x000F000Fu) | 0x43004300u;               // 128 + q
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x43084308u));     // 136
+    return r;
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+struct F16Operand {
+  using T = __half;
+  static __device__ __forceinline__ uint32_t pair(uint32_t w) {
+    const uint32_t biased = (w & 0x000F000Fu) | 0x64006400u;               // 1024 + q
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x64086408u));      // 1032
+    return r;
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <typename X> struct OperandOf { using type = Bf16Operand; static constexpr int parts = 1; };
+template <> struct OperandOf<__half> { using type = F16Operand; static constexpr int parts = 1; };
+template <> struct OperandOf<float> { using type = Bf16Operand; static constexpr int parts = 3; };
+
+// part `k` of x as an operand
+__device__ __forceinline__ __nv_bfloat16 part_of(__nv_bfloat16 x, int) { return x; }
+__device__ __forceinline__ __half part_of(__half x, int) { return x; }
+__device__ __forceinline__ __nv_bfloat16 part_of(float x, int k) {
+  if (!(fabsf(x) <= 3.402823466e38f)) return __float2bfloat16_rn(k == 0 ? x : 0.0f);
+  for (; k > 0; --k) x -= __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);     // cut, not rounded: what is left is exact
+  return __float2bfloat16_rn(__uint_as_float(__float_as_uint(x) & 0xFFFF0000u));
+}
+
+__device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y) {
+  if (type == MONO_F32) static_cast<float*>(to)[i] = y;
+  else if (type == MONO_BF16) static_cast<__nv_bfloat16*>(to)[i] = from_float<__nv_bfloat16>(y);
+  else static_cast<__half*>(to)[i] = from_float<__half>(y);
+}
+
+template <int BYTES> struct Words { uint32_t w[BYTES / 4]; };
+template <int BYTES>
+__device__ __forceinline__ Words<BYTES> load_words(const uint8_t* at, bool there) {
+  Words<BYTES> r = {};
+  if (there) {
+    if constexpr (BYTES == 16) { const uint4 x = __ldg(reinterpret_cast<const uint4*>(at)); r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w; }
+    else if constexpr (BYTES == 8) { const uint2 x = __ldg(reinterpret_cast<const uint2*>(at)); r.w[0] = x.x; r.w[1] = x.y; }
+    else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
+  }
+  return r;
+}
+
+// Columns of `columns` operands (vectors, or the parts of vectors) from x0 on.  Shared memory: [words of a row][columns][4 threads][4 pairs], then the sums of
+// the warps, [warps][16][8 * NT].
+template <typename X, typename S, int GROUP, int NT, int THREADS>
+__global__ void __launch_bounds__(THREADS) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type, int64_t out_stride,
+                                                                 int split, int64_t tiles) {
+  after_previous_kernel();
+  using Op = typename OperandOf<X>::type;
+  constexpr int PARTS = OperandOf<X>::parts;
+  constexpr int BYTES = GROUP / 8, WORDS = BYTES / 4;       // of a row's group, a thread's quarter
+  constexpr int U = GROUP == 128 ? 4 : GROUP == 64 ? 4 : 8;  // groups in flight
+  constexpr int WARPS = THREADS / 32, N = 8 * NT;
+  extern __shared__ uint4 shared[];
+  const int columns = vectors * PARTS;
+  const int row_words = p.groups * WORDS;                   // of a thread's quarter
+  uint4* operands = shared;                                 // [row_words][columns][4]
+  float* sums = reinterpret_cast<float*>(shared + (int64_t)row_words * columns * 4);
+
+  for (int i = threadIdx.x; i < row_words * columns * 4; i += THREADS) {
+    const int t = i % 4, col = i / 4 % columns, w = i / 4 / columns;
+    const int c0 = (w / WORDS) * GROUP + t * (GROUP / 4) + w % WORDS * 8;
+    const X* from = x + (col / PARTS) * x_stride;
+    typename Op::T e[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = c0 + k + 4 * h;
+        e[2 * k + h] = c < p.cols ? part_of(from[c], col % PARTS) : from_float<typename Op::T>(0.0f);
+      }
+    }
+    operands[i] = *reinterpret_cast<const uint4*>(e);
+  }
+  __syncthreads();
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+  const int share = warp % split, team = warp / split, teams = WARPS / split;
+  const int per = (p.groups + split - 1) / split;
+  const int g0 = share * per, g1 = min(g0 + per, p.groups);
+  const int64_t row_bytes = (int64_t)((p.cols + 31) / 32) * 16;
+
+  for (int64_t first = (int64_t)blockIdx.x * teams; first < tiles; first += (int64_t)gridDim.x * teams) {
+    const int64_t row0 = (first + team) * kTileRows;
+    const int64_t ra = min(row0 + g, p.rows - 1), rb = min(row0 + g + 8, p.rows - 1);
+    const uint8_t *qa = p.q + ra * p.q_stride + t * BYTES, *qb = p.q + rb * p.q_stride + t * BYTES;
+    const S *sa = static_cast<const S*>(p.scales) + ra * p.scale_stride, *sb = static_cast<const S*>(p.scales) + rb * p.scale_stride;
+    float total[NT][4] = {};
+    if (row0 < p.rows) {
+      for (int k0 = g0; k0 < g1; k0 += U) {
+        Words<BYTES> wa[U], wb[U];
+        float fa[U], fb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int k = k0 + u;
+          const bool there = k < g1 && (int64_t)k * (GROUP / 2) + (t + 1) * BYTES <= row_bytes;
+          wa[u] = load_words<BYTES>(qa + k * (GROUP / 2), there);
+          wb[u] = load_words<BYTES>(qb + k * (GROUP / 2), there);
+          fa[u] = k < g1 ? to_float(sa[k]) : 0.0f;
+          fb[u] = k < g1 ? to_float(sb[k]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int k = k0 + u;
+          if (k >= g1) break;
+          float sum[NT][4] = {};
+#pragma unroll
+          for (int w = 0; w < WORDS; ++w) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              a[h][0] = Op::pair(wa[u].w[w] >> (8 * h));
+              a[h][1] = Op::pair(wb[u].w[w] >> (8 * h));
+              a[h][2] = Op::pair(wa[u].w[w] >> (8 * h + 4));
+              a[h][3] = Op::pair(wb[u].w[w] >> (8 * h + 4));
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              uint4 b = make_uint4(0, 0, 0, 0);
+              if (nt * 8 + g < columns) b = operands[((int64_t)(k * WORDS + w) * columns + nt * 8 + g) * 4 + t];
+              Op::mma(sum[nt], a[0], b.x, b.y);
+              Op::mma(sum[nt], a[1], b.z, b.w);
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            total[nt][0] += fa[u] * sum[nt][0];
+            total[nt][1] += fa[u] * sum[nt][1];
+            total[nt][2] += fb[u] * sum[nt][2];
+            total[nt][3] += fb[u] * sum[nt][3];
+          }
+        }
+      }
+    }
+    float* mine = sums + warp * kTileRows * N;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      mine[g * N + nt * 8 + 2 * t] = total[nt][0];
+      mine[g * N + nt * 8 + 2 * t + 1] = total[nt][1];
+      mine[(g + 8) * N + nt * 8 + 2 * t] = total[nt][2];
+      mine[(g + 8) * N + nt * 8 + 2 * t + 1] = total[nt][3];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < teams * kTileRows * vectors; i += THREADS) {
+      const int r = i % (teams * kTileRows), m = i / (teams * kTileRows);
+      const int64_t row = first * kTileRows + r;
+      if (row >= p.rows) continue;
+      float y = 0.0f;
+      for (int w = 0; w < split; ++w)
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k)                // (the small parts first)
+          y += sums[((r / kTileRows * split + w) * kTileRows + r % kTileRows) * N + m * PARTS + k];
+      store_as(out, out_type, m * out_stride + row, y);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename X, typename S, int GROUP, int NT, int THREADS>
+int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int vectors, void* out, int out_type, int64_t out_stride, cudaStream_t s) {
+  constexpr int WARPS = THREADS / 32, N = 8 * NT;
+  auto* kernel = packed_scores_kernel<X, S, GROUP, NT, THREADS>;
+  const int columns = vectors * OperandOf<X>::parts;
+  const size_t shared = (size_t)p.groups * (GROUP / 32) * columns * 64 + (size_t)WARPS * kTileRows * N * 4;
+  int split = 1;
+  while (split < WARPS && p.groups >= split * 2 * 4) split *= 2;
+  const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows;
+  const int teams = WARPS / split;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) return MONO_ERR_CUDA;
+  int blocks = 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, THREADS, shared) != cudaSuccess || blocks < 1) return MONO_ERR_CUDA;
+  const int64_t grid = std::min<int64_t>((tiles + teams - 1) / teams, 148ll * blocks);
+  return launch_operator(kernel, dim3((unsigned)grid), THREADS, shared, s, p, x, x_stride, vectors, out, out_type, out_stride, split, tiles);
+}
+
+template <typename X, typename S, int GROUP>
+int launch_scores(const mono_packed_t& packed, const mono_matrix_t& x, const mono_matrix_t& out, cudaStream_t s) {
+  constexpr int PARTS = OperandOf<X>::parts;
+  const PackedView p = view(packed);
+  const int64_t operand_bytes = (int64_t)p.groups * GROUP * 2;                    // of one operand vector in shared memory
+  // vectors of a launch: up to 16 operands, and no more than shared memory has room for
+  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(16 / PARTS, (200 * 1024) / (operand_bytes * PARTS)));
+  for (int64_t m = 0; m < x.rows; m += most) {
+    const int vectors = (int)std::min<int64_t>(most, x.rows - m);
+    const X* from = static_cast<const X*>(x.data) + m * x.stride;
+    char* to = static_cast<char*>(out.data) + m * out.stride * element_size(out.type);
+    const int rc = vectors * PARTS <= 8 ? launch_scores_tile<X, S, GROUP, 1, kThreads>(p, from, x.stride, vectors, to, out.type, out.stride, s)
+                                        : launch_scores_tile<X, S, GROUP, 2, kThreads>(p, from, x.stride, vectors, to, out.type, out.stride, s);
+    if (rc != MONO_OK) return rc;
+  }
+  return MONO_OK;
+}
+
+template <typename F>
+int with_group(int group, F&& f) {
+  return group == 32 ? f(Width<32>()) : group == 64 ? f(Width<64>()) : f(Width<128>());
+}
+
+}  // namespace
+
+extern "C" {
+
+int mono_pack_rows(const mono_matrix_t* rows, const mono_packed_t* packed, void* cuda_stream) {
+  const OperatorRange range(__func__);
+  if (!matrix_ok(rows, false) || !packed_ok(packed) || rows->rows != packed->rows || rows->cols != packed->cols) return MONO_ERR_ARG;
+  if (packed->rows == 0) return MONO_OK;
+  const PackedView p = view(*packed);
+  const int64_t blocks = (p.rows * p.groups + kThreads / 16 - 1) / (kThreads / 16);
+  if (blocks > INT_MAX) return MONO_ERR_LIMIT;
+  return with_type(rows->type, [&](auto w) {
+    return with_type(packed->scale_type, [&](auto s) {
+      return with_group(packed->group, [&](auto g) {
+        using W = decltype(w);
+        return launch_operator(pack_rows_kernel<W, decltype(s), decltype(g)::value>, dim3((unsigned)blocks), kThreads, 0, static_cast<cudaStream_t>(cuda_stream),
+                               static_cast<const W*>(rows->data), rows->stride, p);
+      });
+    });
+  });
+}
+
+int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int32_t token_type, int64_t n_tokens, int64_t padding, float scale, const mono_matrix_t* out,
+                           void* cuda_stream) {
+  const OperatorRange range(__func__);
+  if (!packed_ok(packed) || !matrix_ok(out, true) || !tokens_ok(tokens, token_type, n_tokens)) return MONO_ERR_ARG;
+  if (out->rows != n_tokens || out->cols != packed->cols) return MONO_ERR_ARG;
+  if (n_tokens == 0) return MONO_OK;
+  const PackedView p = view(*packed);
+  const TokenList list{tokens, n_tokens, packed->rows, padding, token_type == MONO_I64};
+  const int words = (p.cols + 7) / 8;
+  int lanes = 1;
+  while (lanes < 32 && lanes < words) lanes *= 2;
+  const int64_t rows = kThreads / lanes;
+  const dim3 grid((unsigned)((n_tokens + rows - 1) / rows), (unsigned)((words + lanes - 1) / lanes));
+  return with_type(packed->scale_type, [&](auto s) {
+    return with_type(out->type, [&](auto o) {
+      using O = decltype(o);
+      const auto launch = [&](auto* kernel) {
+        return launch_operator(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), p, packed->group / 8, list, scale, static_cast<O*>(out->data), out->stride, lanes);
+      };
+      return vector_of(*out) == 8 ? launch(packed_token_rows_kernel<decltype(s), O, true>) : launch(packed_token_rows_kernel<decltype(s), O, false>);
+    });
+  });
+}
+
+int mono_packed_scores(const mono_packed_t* packed, const mono_matrix_t* x, const mono_matrix_t* out, void* cuda_stream) {
+  const OperatorRange range(__func__);
+  if (!packed_ok(packed) || !matrix_ok(x, false) || !out || out->rows != x->rows || x->cols != packed->cols) return MONO_ERR_ARG;
+  if (x->rows > MONO_MAX_SCORED || x->cols > MONO_MAX_SCORED_COLS) return MONO_ERR_LIMIT;
+  if (out->cols != packed->rows) return MONO_ERR_ARG;
+  if (packed->rows == 0 || x->rows == 0) return MONO_OK;
+  // (a row of scores is as long as there are rows: not a matrix of at most MONO_MAX_COLS columns)
+  const int size = element_size(out->type);
+  if (!size || !out->data || !is_aligned(out->data, size) || out->stride < 0 || out->stride > (int64_t)1 << 40 || (out->rows > 1 && out->stride < out->cols)) return MONO_ERR_ARG;
+  return with_type(x->type, [&](auto xt) {
+    return with_type(packed->scale_type, [&](auto s) {
+      return with_group(packed->group, [&](auto g) {
+        return launch_scores<decltype(xt), decltype(s), decltype(g)::value>(*packed, *x, *out, static_cast<cudaStream_t>(cuda_stream));
+      });
+    });
+  });
+}
+
+}  // extern "C"
