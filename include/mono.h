@@ -531,11 +531,13 @@ int mono_timing_read(mono_table* t, mono_timing_t* host_out, int reset);
  *    and be captured into CUDA graphs.  Descriptors are HOST structs, read before the call returns.
  *  - A matrix that is written must not overlap anything else the call is given.
  *  - Products and sums are taken in fp32, and what is written is rounded once, to nearest even.
- *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS (a row of scores has one per packed row).
+ *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS, strides up to MONO_MAX_STRIDE (a row of
+ *    scores has one column per packed row).
  *  - A token outside [0, vocabulary) has no row: it looks up as zeros and its gradient is dropped, like MONO_RESERVED_ID in
  *    a table.  So does the token `padding` (-1, or any other number outside the vocabulary, for none).
  */
 #define MONO_MAX_COLS 65536
+#define MONO_MAX_STRIDE (1 << 29)
 
 enum { MONO_F32 = 0, MONO_BF16 = 1, MONO_F16 = 2 };   /* types of elements */
 enum { MONO_I32 = 0, MONO_I64 = 1 };                  /* types of tokens, signed */

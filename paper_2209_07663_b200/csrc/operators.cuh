@@ -4,6 +4,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <cstring>
+#include <type_traits>
 #include <utility>
 
 #include <cuda_bf16.h>
@@ -22,7 +24,8 @@ struct OperatorRange {
 };
 
 __device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+// (its bits are the upper half of the float's)
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __uint_as_float((uint32_t)__bfloat16_as_ushort(x) << 16); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 // (to nearest, ties to even: an output is rounded once, here)
 template <typename T> __device__ __forceinline__ T from_float(float x);
@@ -34,6 +37,44 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 template <typename T, int N>
 struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Vec { T v[N]; };
 
+template <typename T, int N>
+__device__ __forceinline__ void to_floats(const Vec<T, N>& x, float (&f)[N]) {
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+    // two at a time: a bf16 pair's upper half is a float already, but for the bits below
+    uint32_t w[N / 2];
+    memcpy(w, &x, sizeof(w));
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        f[2 * k] = __uint_as_float(w[k] << 16);
+        f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      } else {
+        __half2 h;
+        memcpy(&h, &w[k], 4);
+        const float2 p = __half22float2(h);
+        f[2 * k] = p.x;
+        f[2 * k + 1] = p.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = to_float(x.v[k]);
+  }
+}
+
+// sum += x, two columns an instruction
+template <int N>
+__device__ __forceinline__ void add_floats(float (&sum)[N], const float (&x)[N]) {
+  if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2)
+      asm("{.reg .b64 a, b; mov.b64 a, {%0, %1}; mov.b64 b, {%2, %3}; add.rn.f32x2 a, a, b; mov.b64 {%0, %1}, a;}" : "+f"(sum[k]), "+f"(sum[k + 1]) : "f"(x[k]), "f"(x[k + 1]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] += x[k];
+  }
+}
+
 constexpr uint32_t kNoToken = 0xFFFFFFFFu;
 constexpr int64_t kMaxOperatorRows = 0x7FFFFFFEll;      // of a matrix, and tokens of a call
 
@@ -44,10 +85,24 @@ struct TokenList {
   int64_t vocab;
   int64_t padding;
   bool wide;
-  // the row that token i names, or kNoToken: outside the vocabulary, or the padding
+  // the row that a token names, or kNoToken: outside the vocabulary, or the padding
+  __device__ __forceinline__ uint32_t row_of(int64_t t) const { return (uint64_t)t < (uint64_t)vocab && t != padding ? (uint32_t)t : kNoToken; }
   __device__ __forceinline__ uint32_t at(int64_t i) const {
-    const int64_t t = wide ? static_cast<const int64_t*>(data)[i] : static_cast<const int32_t*>(data)[i];
-    return (uint64_t)t < (uint64_t)vocab && t != padding ? (uint32_t)t : kNoToken;
+    return row_of(wide ? static_cast<const int64_t*>(data)[i] : static_cast<const int32_t*>(data)[i]);
+  }
+  // those of the K tokens first, first + step, ... (kNoToken behind the last one), all read before the first is looked at
+  template <int K>
+  __device__ __forceinline__ void rows(int64_t first, int64_t step, uint32_t (&row)[K]) const {
+    int64_t t[K];
+    if (wide) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? __ldg(static_cast<const long long*>(data) + first + k * step) : -1;
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? __ldg(static_cast<const int*>(data) + first + k * step) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) row[k] = row_of(t[k]);
   }
 };
 
@@ -60,7 +115,7 @@ inline bool matrix_ok(const mono_matrix_t* m, bool written) {
   const int size = element_size(m->type);
   if (!size || m->rows < 0 || m->rows > kMaxOperatorRows || m->cols < 1 || m->cols > MONO_MAX_COLS) return false;
   if (m->rows == 0) return true;
-  if (m->stride < 0 || m->stride > (int64_t)1 << 40 || (written && m->rows > 1 && m->stride < m->cols)) return false;
+  if (m->stride < 0 || m->stride > MONO_MAX_STRIDE || (written && m->rows > 1 && m->stride < m->cols)) return false;
   return m->data && is_aligned(m->data, size);
 }
 
@@ -92,19 +147,32 @@ int with_width(int v, F&& f) {
 
 // Launch of a kernel that waits for the stream's previous kernel itself (after_previous_kernel), so that its
 // launch is prepared while that one runs.
+struct Launch {
+  dim3 grid;
+  unsigned block;
+  size_t shared;
+  cudaStream_t stream;
+  unsigned cluster;        // blocks along x, 0: none
+};
+template <typename... P, typename... A>
+inline int launch_operator(const Launch& l, void (*kernel)(P...), A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = l.grid;
+  cfg.blockDim = dim3(l.block, 1, 1);
+  cfg.dynamicSmemBytes = l.shared;
+  cfg.stream = l.stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {l.cluster, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = l.cluster ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess ? MONO_OK : MONO_ERR_CUDA;
+}
 template <typename... P, typename... A>
 inline int launch_operator(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, cudaStream_t s, A&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(block, 1, 1);
-  cfg.dynamicSmemBytes = shared;
-  cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess ? MONO_OK : MONO_ERR_CUDA;
+  return launch_operator(Launch{grid, block, shared, s, 0u}, kernel, std::forward<A>(args)...);
 }
 
 }  // namespace mono

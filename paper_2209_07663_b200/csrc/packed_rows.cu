@@ -21,8 +21,8 @@ inline bool packed_ok(const mono_packed_t* p) {
   if (!p || !element_size(p->scale_type) || (p->group != 32 && p->group != 64 && p->group != 128)) return false;
   if (p->rows < 0 || p->rows > kMaxOperatorRows || p->cols < 1 || p->cols > MONO_MAX_COLS) return false;
   if (p->rows == 0) return true;
-  if (p->q_stride % 16 || p->q_stride < (p->cols + 31) / 32 * 16 || p->q_stride > (int64_t)1 << 40) return false;
-  if (p->scale_stride < (p->cols + p->group - 1) / p->group || p->scale_stride > (int64_t)1 << 40) return false;
+  if (p->q_stride % 16 || p->q_stride < (p->cols + 31) / 32 * 16 || p->q_stride > MONO_MAX_STRIDE) return false;
+  if (p->scale_stride < (p->cols + p->group - 1) / p->group || p->scale_stride > MONO_MAX_STRIDE) return false;
   return p->q && is_aligned(p->q, 16) && p->scales && is_aligned(p->scales, element_size(p->scale_type));
 }
 
@@ -391,7 +391,7 @@ int mono_packed_scores(const mono_packed_t* packed, const mono_matrix_t* x, cons
   if (packed->rows == 0 || x->rows == 0) return MONO_OK;
   // (a row of scores is as long as there are rows: not a matrix of at most MONO_MAX_COLS columns)
   const int size = element_size(out->type);
-  if (!size || !out->data || !is_aligned(out->data, size) || out->stride < 0 || out->stride > (int64_t)1 << 40 || (out->rows > 1 && out->stride < out->cols)) return MONO_ERR_ARG;
+  if (!size || !out->data || !is_aligned(out->data, size) || out->stride < 0 || out->stride > kMaxOperatorRows || (out->rows > 1 && out->stride < out->cols)) return MONO_ERR_ARG;
   return with_type(x->type, [&](auto xt) {
     return with_type(packed->scale_type, [&](auto s) {
       return with_group(packed->group, [&](auto g) {

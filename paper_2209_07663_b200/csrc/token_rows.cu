@@ -26,11 +26,7 @@ __global__ void __launch_bounds__(kThreads) token_rows_kernel(const W* __restric
   const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
   const int v0 = blockIdx.y * lanes * PIECES + lane;
   uint32_t t[ROWS];
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    const int64_t i = row0 + r * groups;
-    t[r] = i < tokens.n ? tokens.at(i) : kNoToken;
-  }
+  tokens.rows(row0, groups, t);
   Vec<W, VEC> in[kMoves];
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
@@ -71,21 +67,485 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
 }
 
 // ---------------------------------------------------------------------------
-// Gradient.  The tokens are sorted stably by row (radix sort, least digit first; tokens without a row last), so that
-// the terms of a row are consecutive; the sorted positions are cut into chunks of kChunk, every chunk adds up its rows in order
-// and writes those that begin and end in it.  What a row has in a chunk that it does not begin and end in is a partial
-// sum in the workspace: `head` if it began in an earlier chunk, `tail` if it begins here; join_rows_kernel adds
-// a row's tail and heads.  All orders follow from the sorted tokens, so the result has the same bits every time.
+// Gradient.  The tokens are sorted stably by row (tokens without a row last), so that the terms of a row are
+// consecutive.  A group of up to 32 threads adds up a run of sorted positions in order and writes the rows that begin and end in
+// it; what it has of other rows, a piece in front and a piece at the end, a block joins over its groups' runs in
+// shared memory, and join_rows_kernel over the blocks, both in the order of the positions.  The terms are read once and
+// no order depends on timing, so the result has the same bits every time.
+//
+// Three ways to sort, by the number of tokens:
+//   up to kSmallTokens   every block of the summing kernel ranks all tokens in shared memory: no launch of its own
+//   up to kRankTokens    one launch: a token's place is the number of tokens before it, counted; n * n comparisons
+//   beyond               radix sort, least digit first, two launches a digit of up to 9 bits
+// Where all of the gradient is written, its zeros are filled in by blocks behind those that sort, which
+// use a few SMs for a few microseconds; the rows that tokens name are written again by the sums.
 // ---------------------------------------------------------------------------
-constexpr int kChunk = 64;
-constexpr int kSortThreads = 256;
+constexpr int64_t kSmallTokens = 256;
+constexpr int64_t kRankTokens = 8192;
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortKeys = 8;                               // keys of a thread
 constexpr int kSortTile = kSortThreads * kSortKeys;
 constexpr int kMaxDigitBits = 9;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
-constexpr int kCoarse = 16;                                // tiles whose digit counts are also kept summed up
+static_assert(kMaxDigits == kSortThreads, "a thread has one digit's counts");
+constexpr int64_t kMaxFineTiles = 64;                      // beyond, the digits' counts are also summed up over kCoarse tiles each
+constexpr int kCoarse = 32;
+constexpr int kLaneColumns = 8;                            // columns whose sums a thread holds
+constexpr int kMinRun = 8, kMaxRun = 64;                   // positions of a group
 
 struct Entry { uint32_t row, at; };                        // a token's row (vocab: none) and its position
+constexpr uint32_t kBehind = 0xFFFFFFFFu;                  // row of the entry behind the last one
+
+// Zeros of rows [begin, end) of the matrix that is written, but for the rows that are marked as named by a token: a group of `lanes`
+// threads has four rows at a time.
+struct Zeros {
+  char* data;
+  int64_t stride;          // bytes from a row to the next
+  int64_t begin, end;
+  int pieces, size;        // of a row, and bytes of one: as many as the row's alignment allows
+  int lanes;
+  const uint8_t* marks;    // nullptr: none is
+  unsigned first;          // the block that begins
+
+  __device__ __forceinline__ bool here() const { return blockIdx.x >= first; }
+
+  template <typename T>
+  __device__ __forceinline__ void rows() const {
+    const int lane = threadIdx.x & (lanes - 1), groups = blockDim.x / lanes;
+    const int64_t step = (int64_t)(gridDim.x - first) * groups * 4;
+    for (int64_t r0 = begin + ((int64_t)(blockIdx.x - first) * groups + threadIdx.x / lanes) * 4; r0 < end; r0 += step) {
+      bool write[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) write[k] = r0 + k < end && !(marks && marks[r0 + k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (!write[k]) continue;
+        T* row = reinterpret_cast<T*>(data + (r0 + k) * stride);
+        for (int i = lane; i < pieces; i += lanes) row[i] = T{};
+      }
+    }
+  }
+  __device__ void fill() const {
+    if (size == 16) rows<uint4>(); else if (size == 8) rows<uint2>(); else if (size == 4) rows<uint32_t>(); else rows<uint16_t>();
+  }
+};
+
+// The tokens of a call: the caller's in the first pass, the entries of the pass before in the others.
+struct Keys {
+  TokenList tokens;
+  const Entry* entries;    // nullptr: the tokens
+  // those at first, first + step, ... (none behind the last one: kBehind)
+  template <int K>
+  __device__ __forceinline__ void load(int64_t first, int64_t step, Entry (&e)[K]) const {
+    if (entries) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint2 x = first + k * step < tokens.n ? __ldg(reinterpret_cast<const uint2*>(entries) + first + k * step) : make_uint2(kBehind, 0);
+        e[k] = {x.x, x.y};
+      }
+      return;
+    }
+    uint32_t row[K];
+    tokens.rows(first, step, row);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t i = first + k * step;
+      e[k] = {i >= tokens.n ? kBehind : row[k] == kNoToken ? (uint32_t)tokens.vocab : row[k], (uint32_t)i};
+    }
+  }
+};
+
+// How many of the keys [from, to) in shared memory come before a key: those below it, and of those equal to it the ones at lower positions.
+__device__ __forceinline__ uint32_t count_before(const uint32_t* keys, int from, int to, uint32_t key, int position) {
+  uint32_t n = 0;
+  const int equal_to = min(max(position, from), to);
+#pragma unroll 8
+  for (int j = from; j < equal_to; ++j) n += keys[j] <= key;
+#pragma unroll 8
+  for (int j = equal_to; j < to; ++j) n += keys[j] < key;
+  return n;
+}
+
+// 32 tokens a block; each warp counts over its share of all tokens.
+__global__ void __launch_bounds__(kThreads) rank_tokens_kernel(TokenList tokens, Entry* __restrict__ sorted, Zeros zeros) {
+  after_previous_kernel();
+  if (zeros.here()) { zeros.fill(); return; }
+  constexpr int kWarps = kThreads / 32;
+  __shared__ uint32_t keys[kRankTokens];
+  __shared__ uint32_t counts[kWarps][32];
+  const Keys all{tokens, nullptr};
+  const int n = (int)tokens.n, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kThreads) {
+    Entry e[8];
+    all.load(i0, kThreads, e);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k * kThreads < n) keys[i0 + k * kThreads] = e[k].row;
+  }
+  __syncthreads();
+  const int mine = blockIdx.x * 32 + lane, share = (n + kWarps - 1) / kWarps;
+  const int from = min(warp * share, n), to = min(from + share, n);
+  counts[warp][lane] = mine < n ? count_before(keys, from, to, keys[mine], mine) : 0;
+  __syncthreads();
+  if (warp != 0 || mine >= n) return;
+  uint32_t place = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) place += counts[w][lane];
+  sorted[place] = {keys[mine], (uint32_t)mine};
+  if (mine == 0) sorted[n] = {kBehind, 0};
+}
+
+// (marks: cleared, by the blocks that would fill zeros, where this is the first pass)
+__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, int64_t n, int shift, int bits, uint32_t* __restrict__ counts, uint4* marks, int64_t mark_words,
+                                                                    Zeros zeros) {
+  after_previous_kernel();
+  if (zeros.here()) {
+    if (!marks) { zeros.fill(); return; }
+    for (int64_t i = (int64_t)(blockIdx.x - zeros.first) * kSortThreads + threadIdx.x; i < mark_words; i += (int64_t)(gridDim.x - zeros.first) * kSortThreads)
+      marks[i] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  __shared__ uint32_t count[kMaxDigits];
+  count[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+  Entry e[kSortKeys];
+  keys.load(base + threadIdx.x, kSortThreads, e);
+#pragma unroll
+  for (int k = 0; k < kSortKeys; ++k)
+    if (e[k].row != kBehind) atomicAdd(&count[(e[k].row >> shift) & ((1 << bits) - 1)], 1u);
+  __syncthreads();
+  counts[(int64_t)blockIdx.x * kMaxDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+// counts summed up over kCoarse tiles each
+__global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t* __restrict__ counts, int64_t tiles, uint32_t* __restrict__ coarse) {
+  after_previous_kernel();
+  const int64_t first = (int64_t)blockIdx.x * kCoarse, last = first + kCoarse < tiles ? first + kCoarse : tiles;
+  uint32_t sum = 0;
+#pragma unroll 16
+  for (int64_t t = first; t < last; ++t) sum += counts[t * kMaxDigits + threadIdx.x];
+  coarse[(int64_t)blockIdx.x * kMaxDigits + threadIdx.x] = sum;
+}
+
+// A key goes behind the keys of lower digits of all tiles, those of its digit in earlier tiles, in earlier warps of its tile (warp w has the
+// tile's keys [w * 256, (w + 1) * 256)), in earlier rounds of 32 keys, and at lower lanes (__match_any_sync).
+__global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, int64_t n, int shift, int bits, const uint32_t* __restrict__ counts, int64_t tiles,
+                                                                    const uint32_t* __restrict__ coarse, Entry* __restrict__ sorted, uint8_t* marks, Zeros zeros) {
+  after_previous_kernel();
+  if (zeros.here()) { zeros.fill(); return; }
+  __shared__ __align__(8) uint32_t next[kSortWarps][kMaxDigits];        // counts of the warps, then the place of a warp's next key of a digit
+  __shared__ uint32_t warp_sum[kSortWarps];
+  const int digits = 1 << bits, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int64_t tile = blockIdx.x, base = tile * kSortTile + warp * (32 * kSortKeys);
+  if (tile == 0 && threadIdx.x == 0) sorted[n] = {kBehind, 0};
+  Entry e[kSortKeys];
+  keys.load(base + lane, 32, e);
+  if (marks) {
+    // Of the tile's keys that share a cell, the last one to write it marks its row and those of the same row leave it alone: marked by every
+    // token, the row that a tenth of them name took longer than the rest of the sort.
+    uint64_t* cell = reinterpret_cast<uint64_t*>(next[0]);
+    constexpr uint32_t kCells = sizeof(next) / 8;
+#pragma unroll
+    for (int k = 0; k < kSortKeys; ++k)
+      if (e[k].row < keys.tokens.vocab) cell[e[k].row % kCells] = (uint64_t)e[k].row << 32 | (threadIdx.x * kSortKeys + k);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortKeys; ++k) {
+      if (e[k].row >= keys.tokens.vocab) continue;
+      const uint64_t by = cell[e[k].row % kCells];
+      if ((uint32_t)(by >> 32) != e[k].row || (uint32_t)by == threadIdx.x * kSortKeys + k) marks[e[k].row] = 1;
+    }
+    __syncthreads();
+  }
+  // of this thread's digit: keys of all tiles, and of earlier ones
+  uint32_t total = 0, before = 0;
+  if (coarse == nullptr) {
+#pragma unroll 16
+    for (int64_t t = 0; t < tiles; ++t) {
+      const uint32_t c = counts[t * kMaxDigits + threadIdx.x];
+      total += c;
+      if (t < tile) before += c;
+    }
+  } else {
+    const int64_t own = tile / kCoarse, n_coarse = (tiles + kCoarse - 1) / kCoarse;
+#pragma unroll 16
+    for (int64_t t = 0; t < n_coarse; ++t) {
+      const uint32_t c = coarse[t * kMaxDigits + threadIdx.x];
+      total += c;
+      if (t < own) before += c;
+    }
+#pragma unroll 16
+    for (int64_t t = own * kCoarse; t < tile; ++t) before += counts[t * kMaxDigits + threadIdx.x];
+  }
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) next[w][threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSortKeys; ++k)
+    if (e[k].row != kBehind) atomicAdd(&next[warp][(e[k].row >> shift) & (digits - 1)], 1u);
+  uint32_t scan = total;
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) {
+    const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, scan, s);
+    if (lane >= s) scan += x;
+  }
+  if (lane == 31) warp_sum[warp] = scan;
+  __syncthreads();
+  uint32_t place = scan - total + before;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) place += w < warp ? warp_sum[w] : 0;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) {
+    const uint32_t c = next[w][threadIdx.x];
+    next[w][threadIdx.x] = place;
+    place += c;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSortKeys; ++k) {
+    const bool there = e[k].row != kBehind;
+    const uint32_t digit = there ? (e[k].row >> shift) & (digits - 1) : kMaxDigits;
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+    const uint32_t rank = __popc(same & ((1u << lane) - 1));
+    uint32_t to = 0;
+    if (there) to = next[warp][digit] + rank;
+    __syncwarp();
+    if (there && rank == 0) next[warp][digit] += __popc(same);
+    __syncwarp();
+    if (there && to < n) sorted[to] = e[k];
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) zero_rows_kernel(Zeros zeros) {
+  after_previous_kernel();
+  zeros.fill();
+}
+
+// Where the sums of a call go.
+template <typename O>
+struct GradOut {
+  O* data;
+  int64_t stride;
+  float* partial;          // [blocks][2][cols]: of the row that began in an earlier block, of the one that goes on in the next
+  int cols;
+  uint32_t vocab;
+  float scale;
+};
+
+// ADD: what is there is added to.  It is read with the terms, ahead of the sum that it waits for: a row at a time, a
+// thread's reads would come one after the other.
+// blockIdx.x: runs of `run` positions, one for each group of `lanes` threads; blockIdx.y: part_vectors vectors of VEC columns.
+// Without `sorted` (at most kSmallTokens tokens, all in the runs of one block) the block sorts the tokens itself.
+template <typename G, typename O, int VEC, bool ADD>
+__global__ void __launch_bounds__(kThreads, VEC >= 4 && !ADD ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
+                                                                                       int run, GradOut<O> out, int part_vectors, int lanes) {
+  after_previous_kernel();
+  constexpr int R = kLaneColumns / VEC;
+  constexpr int U = 4;      // positions whose terms are in flight at once
+  constexpr uint32_t kNone = 0xFFFFFFFFu;
+  __shared__ float piece[2 * kThreads * kLaneColumns];      // [groups][2][lanes * kLaneColumns]: front, end
+  __shared__ uint2 pieces[2 * kThreads];                    // of the pieces there are, in order: the row, the place in piece[]
+  __shared__ uint32_t warp_pieces[kThreads / 32];
+  __shared__ uint32_t keys[kSmallTokens];
+  __shared__ Entry ranked[kSmallTokens + 1];
+  const int64_t n = tokens.n;
+  if (sorted == nullptr) {
+    const Keys all{tokens, nullptr};
+    Entry own[1];
+    all.load(threadIdx.x, 1, own);
+    keys[threadIdx.x] = own[0].row;
+    __syncthreads();
+    if (threadIdx.x < n) ranked[count_before(keys, 0, (int)n, keys[threadIdx.x], threadIdx.x)] = {keys[threadIdx.x], threadIdx.x};
+    if (threadIdx.x == 0) ranked[n] = {kBehind, 0};
+    __syncthreads();
+    sorted = ranked;
+  }
+  const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes, width = lanes * kLaneColumns;
+  const int64_t b0 = (int64_t)blockIdx.x * groups * run, b1 = b0 + (int64_t)groups * run < n ? b0 + (int64_t)groups * run : n;
+  const int64_t p0 = b0 + (int64_t)group * run;
+  const int first = blockIdx.y * part_vectors, end = min(first + part_vectors, out.cols / VEC);
+  uint32_t front_row = kNone, end_row = kNone;
+  const Entry* const list = sorted + p0;
+  int len = (int)max((int64_t)0, min(b1 - p0, (int64_t)run));
+  if (len > 0 && list[len - 1].row >= out.vocab) {          // not those without a row: they are last
+    if (list[0].row >= out.vocab) len = 0;
+    while (len > 0 && list[len - 1].row >= out.vocab) --len;
+  }
+
+  if (len > 0) {
+    float sum[R][VEC] = {};
+    bool mine[R];                                           // vectors that there are
+#pragma unroll
+    for (int r = 0; r < R; ++r) mine[r] = first + lane + r * lanes < end;
+    const char* const from = reinterpret_cast<const char*>(grad) + (int64_t)(first + lane) * (VEC * sizeof(G));
+    O* const to = out.data + (int64_t)(first + lane) * VEC;
+    Entry e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) e[u] = list[min(u, len)];
+    bool began_before = p0 > 0 && list[-1].row == e[0].row;
+
+    for (int i = 0; i < len; i += U) {
+      Vec<G, VEC> term[U][R];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const char* row = from + (uint64_t)e[u].at * grad_stride;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (i + u < len && mine[r]) term[u][r] = *reinterpret_cast<const Vec<G, VEC>*>(row + r * lanes * (int)(VEC * sizeof(G)));
+      }
+      Entry ahead[U];                                       // the next positions, while the terms are on their way
+#pragma unroll
+      for (int u = 0; u < U; ++u) ahead[u] = list[min(i + U + u, len)];
+      uint32_t last = 0;                                    // positions that are the last ones of their rows
+#pragma unroll
+      for (int u = 0; u < U; ++u) last |= (e[u].row != (u + 1 < U ? e[u + 1] : ahead[0]).row ? 1u : 0u) << u;
+      Vec<O, VEC> old[ADD ? U : 1][R];
+      if constexpr (ADD) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const O* at = to + (int64_t)e[u].row * out.stride;
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (i + u < len && (last >> u & 1) && mine[r]) old[u][r] = *reinterpret_cast<const Vec<O, VEC>*>(at + r * lanes * VEC);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u < len) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            float f[VEC];
+            to_floats(term[u][r], f);
+            add_floats(sum[r], f);
+          }
+          const bool ends = last >> u & 1;
+          if (ends || i + u + 1 == len) {
+            if (ends && !began_before) {
+              O* at = to + (int64_t)e[u].row * out.stride;
+#pragma unroll
+              for (int r = 0; r < R; ++r) {
+                Vec<O, VEC> o;
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) {
+                  if constexpr (ADD) o.v[c] = from_float<O>(to_float(old[u][r].v[c]) + out.scale * sum[r][c]);
+                  else o.v[c] = from_float<O>(out.scale * sum[r][c]);
+                }
+                if (mine[r]) *reinterpret_cast<Vec<O, VEC>*>(at + r * lanes * VEC) = o;
+              }
+            } else {
+              float* keep = piece + (group * 2 + (began_before ? 0 : 1)) * width + lane * VEC;
+#pragma unroll
+              for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) keep[r * lanes * VEC + c] = sum[r][c];
+              }
+              if (began_before) front_row = e[u].row; else end_row = e[u].row;
+            }
+            began_before = false;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+              for (int c = 0; c < VEC; ++c) sum[r][c] = 0.0f;
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) e[u] = ahead[u];
+    }
+  }
+
+  // the groups' pieces in order; those of one row follow one another
+  {
+    const int mine = lane == 0 ? (front_row != kNone) + (end_row != kNone) : 0, in_warp = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int scan = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, scan, s);
+      if (in_warp >= s) scan += x;
+    }
+    if (in_warp == 31) warp_pieces[warp] = scan;
+    __syncthreads();
+    int at = scan - mine;
+    for (int w = 0; w < warp; ++w) at += warp_pieces[w];
+    if (lane == 0 && front_row != kNone) pieces[at++] = make_uint2(front_row, (group * 2) * width);
+    if (lane == 0 && end_row != kNone) pieces[at] = make_uint2(end_row, (group * 2 + 1) * width);
+    __syncthreads();
+  }
+  int count = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) count += warp_pieces[w];
+  if (count == 0) return;
+  const uint32_t before_row = b0 > 0 ? sorted[b0 - 1].row : kNone, behind_row = b1 < n ? sorted[b1].row : kNone;
+  for (int c = threadIdx.x; c < (end - first) * VEC; c += kThreads) {
+    constexpr int K = 8;
+    const int column = first * VEC + c;
+    float sum = 0.0f;
+    for (int k0 = 0; k0 < count; k0 += K) {
+      uint2 x[K + 1];
+      float part[K], old[K];
+#pragma unroll
+      for (int k = 0; k <= K; ++k) x[k] = k0 + k < count ? pieces[k0 + k] : make_uint2(kNone, 0);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        part[k] = x[k].x != kNone ? piece[x[k].y + c] : 0.0f;
+        if (ADD && x[k].x != x[k + 1].x && x[k].x != before_row && x[k].x != behind_row) old[k] = to_float(out.data[x[k].x * out.stride + column]);
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (x[k].x == kNone) continue;
+        sum += part[k];
+        if (x[k].x == x[k + 1].x) continue;
+        if (x[k].x == before_row) out.partial[(int64_t)blockIdx.x * 2 * out.cols + column] = sum;
+        else if (x[k].x == behind_row) out.partial[((int64_t)blockIdx.x * 2 + 1) * out.cols + column] = sum;
+        else out.data[x[k].x * out.stride + column] = from_float<O>(ADD ? old[k] + out.scale * sum : out.scale * sum);
+        sum = 0.0f;
+      }
+    }
+  }
+}
+
+// A row that begins in block blockIdx.x of the sums (of `positions` sorted positions) and goes on behind it: its partial sums, in order.
+// A thread has VEC columns.
+template <typename O, int VEC>
+__global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* __restrict__ sorted, int64_t n, int positions, bool add, GradOut<O> out) {
+  after_previous_kernel();
+  constexpr int U = 16;
+  const int64_t b = blockIdx.x, p0 = b * positions, p1 = p0 + positions;
+  const uint32_t row = sorted[p1].row, last = sorted[p1 - 1].row, before = p0 > 0 ? sorted[p0 - 1].row : kBehind;
+  if (row >= out.vocab || last != row || before == row) return;      // (before: it began earlier)
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (c >= out.cols) return;
+  using Part = Vec<float, VEC>;
+  const auto part = [&](int64_t at) { return *reinterpret_cast<const Part*>(out.partial + at * out.cols + c); };
+  Part sum = part(b * 2 + 1);
+  Vec<O, VEC>* const to = reinterpret_cast<Vec<O, VEC>*>(out.data + row * out.stride + c);
+  Vec<O, VEC> o;
+  if (add) o = *to;
+  const int64_t blocks = (n + positions - 1) / positions;
+  bool goes_on = true;
+  for (int64_t k = b + 1; goes_on; k += U) {
+    Part x[U];
+    uint32_t r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = k + u < blocks ? sorted[(k + u) * positions].row : kBehind;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k + u < blocks) x[u] = part((k + u) * 2);       // (of a block of another row: not used)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      goes_on = goes_on && r[u] == row;
+      if (goes_on) add_floats(sum.v, x[u].v);
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) o.v[v] = from_float<O>(add ? to_float(o.v[v]) + out.scale * sum.v[v] : out.scale * sum.v[v]);
+  *to = o;
+}
+
+// ---- host side ----
 
 struct SortPlan {
   int passes, bits;                                        // digits of `bits` bits each
@@ -99,7 +559,29 @@ SortPlan plan_sort(int64_t n, int64_t vocab) {
   p.passes = (width + kMaxDigitBits - 1) / kMaxDigitBits;
   p.bits = (width + p.passes - 1) / p.passes;
   p.tiles = (n + kSortTile - 1) / kSortTile;
-  p.coarse = (p.tiles + kCoarse - 1) / kCoarse;
+  p.coarse = p.tiles > kMaxFineTiles ? (p.tiles + kCoarse - 1) / kCoarse : 0;
+  return p;
+}
+
+// How the sums are cut: positions of a group, and of a block.
+struct SumPlan {
+  int lanes, groups, parts, part_vectors, run;
+  int64_t blocks;
+};
+
+SumPlan plan_sums(int64_t n, int vectors, int vec) {
+  SumPlan p;
+  const int most = 32 * (kLaneColumns / vec);
+  p.parts = (vectors + most - 1) / most;
+  p.part_vectors = (vectors + p.parts - 1) / p.parts;
+  p.lanes = 1;
+  while (p.lanes < 32 && p.lanes * (kLaneColumns / vec) < p.part_vectors) p.lanes *= 2;
+  p.groups = kThreads / p.lanes;
+  // long runs have fewer pieces, short ones more warps: as long as there are 24 warps for every SM
+  p.run = kMaxRun;
+  while (p.run > kMinRun && n * p.parts / p.run * p.lanes / 32 < 148 * 24) p.run /= 2;
+  if (n <= kSmallTokens) p.run = std::max(1, (int)((n + p.groups - 1) / p.groups));
+  p.blocks = (n + (int64_t)p.run * p.groups - 1) / ((int64_t)p.run * p.groups);
   return p;
 }
 
@@ -108,304 +590,113 @@ struct GradWorkspace {
   Entry* b;
   uint32_t* counts;        // [tiles][digits]
   uint32_t* coarse;        // [coarse][digits]
-  float* partial;          // [chunks][2][cols]: head, tail
+  uint8_t* marks;          // [vocab]: rows that a token names, where the zeros of the others are filled in
+  float* partial;          // [blocks][2][cols]
   int64_t bytes;
 };
 
+// Beyond, the marks would cost more memory than they spare writes.
+constexpr int64_t kMaxMarks = 1 << 24;
+bool marks_rows(int64_t n, int64_t vocab) { return n > kRankTokens && vocab >= kMaxDigits && vocab <= kMaxMarks; }
+
 GradWorkspace carve(char* base, int64_t n, int64_t vocab, int64_t cols) {
-  const SortPlan p = plan_sort(n, vocab);
   int64_t at = 0;
   const auto take = [&](int64_t bytes) { char* r = base + at; at += (bytes + 255) / 256 * 256; return r; };
-  GradWorkspace w;
-  w.a = reinterpret_cast<Entry*>(take(n * (int64_t)sizeof(Entry)));
-  w.b = reinterpret_cast<Entry*>(take(n * (int64_t)sizeof(Entry)));
-  w.counts = reinterpret_cast<uint32_t*>(take(p.tiles * kMaxDigits * 4));
-  w.coarse = reinterpret_cast<uint32_t*>(take(p.coarse * kMaxDigits * 4));
-  w.partial = reinterpret_cast<float*>(take((n + kChunk - 1) / kChunk * 2 * cols * 4));
+  GradWorkspace w = {};
+  if (n > kSmallTokens) {
+    const SortPlan p = plan_sort(n, vocab);
+    w.a = reinterpret_cast<Entry*>(take((n + 1) * (int64_t)sizeof(Entry)));
+    if (n > kRankTokens) {
+      w.b = reinterpret_cast<Entry*>(take((n + 1) * (int64_t)sizeof(Entry)));
+      w.counts = reinterpret_cast<uint32_t*>(take(p.tiles * kMaxDigits * 4));
+      w.coarse = reinterpret_cast<uint32_t*>(take(p.coarse * kMaxDigits * 4));
+      if (marks_rows(n, vocab)) w.marks = reinterpret_cast<uint8_t*>(take(vocab));
+    }
+    int64_t blocks = 0;                                     // (the matrices' alignment decides the vectors)
+    for (int vec = 1; vec <= 8; vec *= 2)
+      if (cols % vec == 0) blocks = std::max(blocks, plan_sums(n, (int)(cols / vec), vec).blocks);
+    w.partial = reinterpret_cast<float*>(take(blocks * 2 * cols * 4));
+  }
   w.bytes = at;
   return w;
 }
 
-// The keys of a tile: from the caller's tokens in the first pass, from the pass before in the others.
-struct Keys {
-  TokenList tokens;
-  const Entry* entries;    // nullptr: the tokens
-  __device__ __forceinline__ Entry at(int64_t i) const {
-    if (entries) return entries[i];
-    const uint32_t t = tokens.at(i);
-    return {t == kNoToken ? (uint32_t)tokens.vocab : t, (uint32_t)i};
-  }
-};
+constexpr unsigned kZeroBlocks = 148 * 4;
 
-__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, int64_t n, int shift, int bits, uint32_t* __restrict__ counts) {
-  after_previous_kernel();
-  __shared__ uint32_t count[kMaxDigits];
-  const int digits = 1 << bits;
-  for (int d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
-#pragma unroll
-  for (int k = 0; k < kSortKeys; ++k) {
-    const int64_t i = base + k * kSortThreads + threadIdx.x;
-    if (i < n) atomicAdd(&count[(keys.at(i).row >> shift) & (digits - 1)], 1u);
-  }
-  __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[(int64_t)blockIdx.x * kMaxDigits + d] = count[d];
-}
-
-// counts summed over kCoarse tiles each
-__global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t* __restrict__ counts, int64_t tiles, int bits, uint32_t* __restrict__ coarse) {
-  after_previous_kernel();
-  const int64_t first = (int64_t)blockIdx.x * kCoarse, last = first + kCoarse < tiles ? first + kCoarse : tiles;
-  for (int d = threadIdx.x; d < 1 << bits; d += kSortThreads) {
-    uint32_t sum = 0;
-    for (int64_t t = first; t < last; ++t) sum += counts[t * kMaxDigits + d];
-    coarse[(int64_t)blockIdx.x * kMaxDigits + d] = sum;
-  }
-}
-
-// Where the tile's keys of each digit go: the keys of lower digits of all tiles, then those of this digit of earlier tiles.
-// Keys keep their order: warp w has the tile's keys [w * 256, (w + 1) * 256), 32 at a time, and a key's place among the equal digits of its 32 is
-// what __match_any_sync says.
-__global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, int64_t n, int shift, int bits, const uint32_t* __restrict__ counts,
-                                                                    const uint32_t* __restrict__ coarse, int64_t n_coarse, Entry* __restrict__ sorted) {
-  after_previous_kernel();
-  constexpr int kWarps = kSortThreads / 32;
-  __shared__ uint32_t next[kWarps][kMaxDigits];             // counts of the warps, then the place of a warp's next key of a digit
-  __shared__ uint32_t warp_sum[kWarps];
-  const int digits = 1 << bits, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t tile = blockIdx.x, base = tile * kSortTile + warp * (32 * kSortKeys);
-  for (int d = threadIdx.x; d < kWarps * kMaxDigits; d += kSortThreads) next[0][d] = 0;
-  __syncthreads();
-  Entry e[kSortKeys];
-#pragma unroll
-  for (int k = 0; k < kSortKeys; ++k) {
-    const int64_t i = base + k * 32 + lane;
-    if (i < n) {
-      e[k] = keys.at(i);
-      atomicAdd(&next[warp][(e[k].row >> shift) & (digits - 1)], 1u);
-    }
-  }
-  // of two digits each (neighbours, so that the scan runs in their order): all keys, and those of earlier tiles
-  constexpr int kPer = kMaxDigits / kSortThreads;
-  uint32_t total[kPer] = {}, before[kPer] = {};
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int d = threadIdx.x * kPer + j;
-    if (d >= digits) continue;
-    for (int64_t c = 0; c < n_coarse; ++c) {
-      const uint32_t x = coarse[c * kMaxDigits + d];
-      total[j] += x;
-      if (c < tile / kCoarse) before[j] += x;
-    }
-    for (int64_t t = tile / kCoarse * kCoarse; t < tile; ++t) before[j] += counts[t * kMaxDigits + d];
-  }
-  uint32_t mine = 0;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) mine += total[j];
-  uint32_t scan = mine;
-#pragma unroll
-  for (int s = 1; s < 32; s *= 2) {
-    const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, scan, s);
-    if (lane >= s) scan += x;
-  }
-  if (lane == 31) warp_sum[warp] = scan;
-  __syncthreads();
-  uint32_t start = scan - mine;
-  for (int w = 0; w < warp; ++w) start += warp_sum[w];
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int d = threadIdx.x * kPer + j;
-    uint32_t place = start + before[j];
-    for (int w = 0; w < kWarps; ++w) {
-      const uint32_t c = next[w][d];
-      next[w][d] = place;
-      place += c;
-    }
-    start += total[j];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kSortKeys; ++k) {
-    const bool there = base + k * 32 + lane < n;
-    const uint32_t digit = there ? (e[k].row >> shift) & (digits - 1) : kMaxDigits;
-    const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-    const uint32_t rank = __popc(same & ((1u << lane) - 1));
-    uint32_t place = 0;
-    if (there) place = next[warp][digit] + rank;
-    __syncwarp();
-    if (there && rank == 0) next[warp][digit] += __popc(same);
-    __syncwarp();
-    if (there && place < n) sorted[place] = e[k];
-  }
-}
-
-template <typename O>
-__global__ void __launch_bounds__(kThreads) zero_rows_kernel(O* __restrict__ out, int64_t stride, int64_t rows, int cols) {
-  after_previous_kernel();
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < cols; c += kThreads) out[r * stride + c] = from_float<O>(0.0f);
-}
-
-template <typename O>
-__device__ __forceinline__ O summed(O* at, float sum, float scale, bool accumulate) {
-  return from_float<O>(accumulate ? to_float(*at) + scale * sum : scale * sum);
-}
-
-// A group of `lanes` threads (a power of two, up to a warp) has one chunk and the columns [first, end) of blockIdx.y's part, in
-// vectors of VEC; a thread holds up to 8 columns' sums.
-template <typename G, typename O, int VEC>
-__global__ void __launch_bounds__(kThreads) sum_rows_kernel(const G* __restrict__ grad, int64_t grad_stride, const Entry* __restrict__ sorted, int64_t n, uint32_t vocab,
-                                                            float scale, bool accumulate, O* __restrict__ out, int64_t out_stride, float* __restrict__ partial,
-                                                            int cols, int part_vectors, int lanes) {
-  after_previous_kernel();
-  constexpr int R = 8 / VEC;
-  constexpr int U = VEC >= 4 ? 8 : 4;                       // positions whose terms are in flight at once
-  const int lane = threadIdx.x & (lanes - 1);
-  const int64_t chunk = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
-  const int64_t p0 = chunk * kChunk, p1 = p0 + kChunk < n ? p0 + kChunk : n;
-  if (p0 >= n) return;
-  const int first = blockIdx.y * part_vectors, end = min(first + part_vectors, cols / VEC);
-  float sum[R][VEC] = {};
-  uint32_t row = sorted[p0].row;
-  if (row >= vocab) return;
-  bool began_before = p0 > 0 && sorted[p0 - 1].row == row;
-
-  const auto flush = [&](bool whole, float* to) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int v = first + lane + r * lanes;
-      if (v < end) {
-        if (whole) {
-          O* at = out + row * out_stride + (int64_t)v * VEC;
-          Vec<O, VEC> o, old;
-          if (accumulate) old = *reinterpret_cast<const Vec<O, VEC>*>(at);
-#pragma unroll
-          for (int c = 0; c < VEC; ++c) o.v[c] = from_float<O>(accumulate ? to_float(old.v[c]) + scale * sum[r][c] : scale * sum[r][c]);
-          *reinterpret_cast<Vec<O, VEC>*>(at) = o;
-        } else {
-#pragma unroll
-          for (int c = 0; c < VEC; ++c) to[v * VEC + c] = sum[r][c];
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) sum[r][c] = 0.0f;
-    }
-  };
-
-  for (int64_t p = p0; p < p1; p += U) {
-    Entry e[U];
-    Vec<G, VEC> term[U][R];
-#pragma unroll
-    for (int u = 0; u < U; ++u) e[u] = p + u < p1 ? sorted[p + u] : Entry{vocab, 0};
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int v = first + lane + r * lanes;
-        if (e[u].row < vocab && v < end) term[u][r] = *reinterpret_cast<const Vec<G, VEC>*>(grad + e[u].at * grad_stride + (int64_t)v * VEC);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (e[u].row >= vocab) continue;                     // behind the chunk's end or the last token with a row
-      if (e[u].row != row) {
-        flush(!began_before, partial + chunk * 2 * cols);
-        row = e[u].row;
-        began_before = false;
-      }
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (first + lane + r * lanes < end) {
-#pragma unroll
-          for (int c = 0; c < VEC; ++c) sum[r][c] += to_float(term[u][r].v[c]);
-        }
-      }
-    }
-  }
-  const bool goes_on = p1 < n && sorted[p1].row == row;
-  flush(!began_before && !goes_on, partial + (chunk * 2 + (began_before ? 0 : 1)) * cols);
-}
-
-// The block of a chunk in which a row begins that goes on behind it adds up the row's partial sums: `ways` of the block's threads
-// take consecutive shares of them for each column, and the shares are added in order.
-template <typename O>
-__global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* __restrict__ sorted, int64_t n, uint32_t vocab, float scale, bool accumulate, O* __restrict__ out,
-                                                             int64_t out_stride, const float* __restrict__ partial, int cols, int lanes) {
-  after_previous_kernel();
-  __shared__ float share[kThreads];
-  const int64_t chunk = blockIdx.x, p0 = chunk * kChunk, p1 = p0 + kChunk;
-  if (p1 >= n) return;
-  const uint32_t row = sorted[p1].row;
-  if (row >= vocab || sorted[p1 - 1].row != row) return;
-  if (sorted[p0].row == row && p0 > 0 && sorted[p0 - 1].row == row) return;       // began earlier
-  // the chunks behind this one whose first token is of this row
-  int64_t low = chunk + 1, high = (n + kChunk - 1) / kChunk;                      // (the first is; `high` is not)
-  while (high - low > 1) {
-    const int64_t mid = (low + high) / 2;
-    if (sorted[mid * kChunk].row == row) low = mid; else high = mid;
-  }
-  const int64_t heads = low - chunk;
-  const int ways = kThreads / lanes, way = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-  const int64_t per = (heads + ways - 1) / ways;
-  const int64_t from = chunk + 1 + way * per, to = min(from + per, chunk + 1 + heads);
-  const int c = blockIdx.y * lanes + lane;
-  float sum = 0.0f;
-  if (c < cols) {
-    if (way == 0) sum = partial[(chunk * 2 + 1) * cols + c];
-#pragma unroll 8
-    for (int64_t k = from; k < to; ++k) sum += partial[k * 2 * cols + c];
-  }
-  share[threadIdx.x] = sum;
-  __syncthreads();
-  if (way != 0 || c >= cols) return;
-  for (int w = 1; w < ways; ++w) sum += share[w * lanes + lane];
-  O* at = out + row * out_stride + c;
-  *at = summed(at, sum, scale, accumulate);
-}
-
-int launch_sort(const TokenList& tokens, const GradWorkspace& w, cudaStream_t s, const Entry** sorted) {
-  const SortPlan p = plan_sort(tokens.n, tokens.vocab);
-  const Entry* from = nullptr;
-  Entry* to = w.a;
-  for (int pass = 0; pass < p.passes; ++pass) {
-    const Keys keys{tokens, from};
-    const int shift = pass * p.bits;
-    int rc;
-    if ((rc = launch_operator(count_digits_kernel, dim3((unsigned)p.tiles), kSortThreads, 0, s, keys, tokens.n, shift, p.bits, w.counts)) != MONO_OK) return rc;
-    if ((rc = launch_operator(sum_counts_kernel, dim3((unsigned)p.coarse), kSortThreads, 0, s, w.counts, p.tiles, p.bits, w.coarse)) != MONO_OK) return rc;
-    if ((rc = launch_operator(scatter_keys_kernel, dim3((unsigned)p.tiles), kSortThreads, 0, s, keys, tokens.n, shift, p.bits, w.counts, w.coarse, p.coarse, to)) != MONO_OK) return rc;
-    from = to;
-    to = to == w.a ? w.b : w.a;
-  }
-  *sorted = from;
-  return MONO_OK;
+Zeros zeros_of(const mono_matrix_t& m) {
+  const int size = element_size(m.type);
+  int bytes = 16;
+  while (bytes > size && (m.cols * size % bytes || !is_aligned(m.data, bytes) || (m.rows > 1 && m.stride * size % bytes))) bytes /= 2;
+  Zeros z = {static_cast<char*>(m.data), m.stride * size, 0, 0, (int)(m.cols * size / bytes), bytes, 1, nullptr, UINT_MAX};
+  while (z.lanes < 32 && z.lanes < z.pieces) z.lanes *= 2;
+  return z;
 }
 
 template <typename G, typename O, int VEC>
 int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale, bool accumulate, const mono_matrix_t& out, const GradWorkspace& w, cudaStream_t s) {
-  const int cols = (int)grad.cols, vectors = cols / VEC;
+  const int cols = (int)out.cols;
+  const int64_t n = tokens.n, vocab = out.rows;
   int rc = MONO_OK;
-  if (!accumulate) {
-    rc = launch_operator(zero_rows_kernel<O>, dim3((unsigned)std::min<int64_t>(out.rows, 148 * 16)), kThreads, 0, s, static_cast<O*>(out.data), out.stride, out.rows, cols);
+  Zeros zeros = zeros_of(out);
+  if (!accumulate && n <= kSmallTokens) {
+    zeros.end = vocab;
+    zeros.first = 0;
+    const int64_t rows = (int64_t)(kThreads / zeros.lanes) * 4;
+    rc = launch_operator(zero_rows_kernel, dim3((unsigned)std::min<int64_t>((vocab + rows - 1) / rows, 148 * 8)), kThreads, 0, s, zeros);
     if (rc != MONO_OK) return rc;
   }
-  if (tokens.n == 0) return MONO_OK;
+  if (n == 0) return MONO_OK;
+  // share `k` of `shares` of the zeros, behind `blocks` blocks that sort
+  const auto share = [&](int k, int shares, int64_t blocks, dim3* grid) {
+    const bool fills = !accumulate && k >= 0;
+    zeros.begin = vocab * k / shares;
+    zeros.end = vocab * (k + 1) / shares;
+    zeros.first = fills ? (unsigned)blocks : UINT_MAX;
+    *grid = dim3((unsigned)blocks + (fills ? kZeroBlocks : 0));
+    return zeros;
+  };
+  const SumPlan sums = plan_sums(n, cols / VEC, VEC);
+  const GradOut<O> to{static_cast<O*>(out.data), out.stride, w.partial, cols, (uint32_t)vocab, scale};
+  const auto* from = static_cast<const G*>(grad.data);
+  const dim3 sum_grid((unsigned)sums.blocks, (unsigned)sums.parts);
   const Entry* sorted = nullptr;
-  if ((rc = launch_sort(tokens, w, s, &sorted)) != MONO_OK) return rc;
-  const int64_t chunks = (tokens.n + kChunk - 1) / kChunk;
-  constexpr int R = 8 / VEC;
-  const int parts = (vectors + 32 * R - 1) / (32 * R), part_vectors = (vectors + parts - 1) / parts;
-  int lanes = 1;
-  while (lanes < 32 && lanes * R < part_vectors) lanes *= 2;
-  const int groups = kThreads / lanes;
-  rc = launch_operator(sum_rows_kernel<G, O, VEC>, dim3((unsigned)((chunks + groups - 1) / groups), (unsigned)parts), kThreads, 0, s, static_cast<const G*>(grad.data), grad.stride,
-                       sorted, tokens.n, (uint32_t)tokens.vocab, scale, accumulate, static_cast<O*>(out.data), out.stride, w.partial, cols, part_vectors, lanes);
-  if (rc != MONO_OK || chunks < 2) return rc;
-  int columns = 1;
-  while (columns < 32 && columns < cols) columns *= 2;
-  return launch_operator(join_rows_kernel<O>, dim3((unsigned)(chunks - 1), (unsigned)((cols + columns - 1) / columns)), kThreads, 0, s, sorted, tokens.n, (uint32_t)tokens.vocab,
-                         scale, accumulate, static_cast<O*>(out.data), out.stride, w.partial, cols, columns);
+  dim3 grid;
+  if (n > kSmallTokens && n <= kRankTokens) {
+    const Zeros z = share(0, 1, (n + 31) / 32, &grid);
+    if ((rc = launch_operator(rank_tokens_kernel, grid, kThreads, 0, s, tokens, w.a, z)) != MONO_OK) return rc;
+    sorted = w.a;
+  } else if (n > kRankTokens) {
+    const SortPlan p = plan_sort(n, vocab);
+    // the first pass clears the marks and sets them, the others fill in the zeros of what is not marked
+    uint8_t* const marks = accumulate || p.passes < 2 ? nullptr : w.marks;
+    const int skipped = marks ? 2 : 0, shares = 2 * p.passes - skipped;
+    Entry* place = w.a;
+    for (int pass = 0; pass < p.passes; ++pass) {
+      const Keys keys{tokens, sorted};
+      const int shift = pass * p.bits;
+      uint8_t* const marked = pass == 0 ? marks : nullptr;
+      zeros.marks = pass == 0 ? nullptr : marks;
+      Zeros z = share(2 * pass - skipped, shares, p.tiles, &grid);
+      if (marked) { z.first = (unsigned)p.tiles; grid = dim3((unsigned)p.tiles + 16); }
+      if ((rc = launch_operator(count_digits_kernel, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, reinterpret_cast<uint4*>(marked), (vocab + 15) / 16, z)) != MONO_OK)
+        return rc;
+      if (p.coarse && (rc = launch_operator(sum_counts_kernel, dim3((unsigned)p.coarse), kSortThreads, 0, s, w.counts, p.tiles, w.coarse)) != MONO_OK) return rc;
+      z = share(2 * pass + 1 - skipped, shares, p.tiles, &grid);
+      if ((rc = launch_operator(scatter_keys_kernel, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, p.tiles, p.coarse ? w.coarse : nullptr, place, marked, z)) != MONO_OK)
+        return rc;
+      sorted = place;
+      place = place == w.a ? w.b : w.a;
+    }
+  }
+  const auto sum = [&](auto* kernel) {
+    return launch_operator(kernel, sum_grid, kThreads, 0, s, from, (uint32_t)(grad.stride * (int64_t)sizeof(G)), tokens, sorted, sums.run, to, sums.part_vectors, sums.lanes);
+  };
+  rc = accumulate ? sum(sum_rows_kernel<G, O, VEC, true>) : sum(sum_rows_kernel<G, O, VEC, false>);
+  if (rc != MONO_OK || sums.blocks < 2) return rc;
+  constexpr int JOINED = std::min(4, VEC);
+  const int joined = cols / JOINED, threads = joined >= kThreads ? kThreads : (joined + 31) / 32 * 32;
+  return launch_operator(join_rows_kernel<O, JOINED>, dim3((unsigned)(sums.blocks - 1), (unsigned)((joined + threads - 1) / threads)), threads, 0, s, sorted, n, sums.run * sums.groups,
+                         accumulate, to);
 }
 
 }  // namespace

@@ -144,7 +144,7 @@ def test_rows_behind_the_32nd_bit():
 
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("dim", [1, 2, 7, 8, 36, 64, 100, 257, 515, 1024])
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 129, 1000, 2049, 5000])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 129, 255, 256, 257, 1000, 2049, 5000, 8192, 8193])
 def test_gradient_of_many_sizes(n, dim, accumulate):
     vocab = (3, 300, 1000)[n % 3]
     for k, (g, o) in enumerate(itertools.product(TYPES, TYPES)):

@@ -113,12 +113,14 @@ def test_null_descriptors_and_flags():
 
 
 def test_workspaces():
-    need = mb.mono_token_rows_grad_workspace(10, 10, 64)
-    assert need > 0
-    assert grad(bytes=need - 1) == mb.MONO_ERR_SIZE
-    assert grad(bytes=-1) == mb.MONO_ERR_SIZE
-    assert grad(workspace=None) == mb.MONO_ERR_ARG
-    assert grad(workspace=DATA + 128) == mb.MONO_ERR_ARG
+    for many in (1000, 10000, 1000000):
+        need = mb.mono_token_rows_grad_workspace(many, 10, 64)
+        assert need > 0
+        sizes = dict(grad_out=matrix(rows=many), n=many)
+        assert grad(bytes=need - 1, **sizes) == mb.MONO_ERR_SIZE
+        assert grad(bytes=-1, **sizes) == mb.MONO_ERR_SIZE
+        assert grad(workspace=None, **sizes) == mb.MONO_ERR_ARG
+        assert grad(workspace=DATA + 128, **sizes) == mb.MONO_ERR_ARG
     n = ctypes.c_int64()
     for bad in ((-1, 10, 64), (10, -1, 64), (10, 10, 0), (10, 10, mb.MONO_MAX_COLS + 1), (1 << 31, 10, 64), (10, 1 << 31, 64)):
         assert lib().mono_token_rows_grad_workspace(*bad, ctypes.byref(n)) == mb.MONO_ERR_ARG
