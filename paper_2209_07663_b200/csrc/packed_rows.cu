@@ -76,26 +76,38 @@ __global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* __restrict
 }
 
 // ---------------------------------------------------------------------------
-// Rows by token of packed rows: a thread makes the 8 columns of one 32-bit word.
+// Rows by token of packed rows.  A thread makes the 8 columns of a 32-bit word, and keeps four words and their scales in flight behind the read
+// of its tokens: four of one row where rows are wide, one of each of four rows where `lanes` threads cover a row.
 // ---------------------------------------------------------------------------
-template <typename S, typename O, bool ALIGNED>
+constexpr int kMoves = 4;
+
+template <typename S, typename O, bool ALIGNED, int ROWS>
 __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView p, int group_words, TokenList tokens, float scale, O* __restrict__ out, int64_t out_stride, int lanes) {
   after_previous_kernel();
-  const int lane = threadIdx.x & (lanes - 1);
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
-  if (i >= tokens.n) return;
-  const uint32_t t = tokens.at(i);
-  const int words = (p.cols + 7) / 8;
-  for (int w = blockIdx.y * lanes + lane; w < words; w += gridDim.y * lanes) {
-    uint32_t q = 0;
-    float s = 0.0f;
-    if (t != kNoToken) {
-      q = *reinterpret_cast<const uint32_t*>(p.q + t * p.q_stride + (int64_t)w * 4);
-      s = to_float(static_cast<const S*>(p.scales)[t * p.scale_stride + w / group_words]);
+  constexpr int PIECES = kMoves / ROWS;
+  const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
+  const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
+  const int words = (p.cols + 7) / 8, w0 = blockIdx.y * lanes * PIECES + lane;
+  uint32_t t[ROWS], q[kMoves];
+  float s[kMoves];
+  tokens.rows(row0, groups, t);
+#pragma unroll
+  for (int k = 0; k < kMoves; ++k) {
+    const uint32_t row = t[k / PIECES];
+    const int w = w0 + (k % PIECES) * lanes;
+    if (row != kNoToken && w < words) {
+      q[k] = __ldg(reinterpret_cast<const uint32_t*>(p.q + row * p.q_stride) + w);
+      s[k] = to_float(static_cast<const S*>(p.scales)[row * p.scale_stride + w / group_words]);
     }
+  }
+#pragma unroll
+  for (int k = 0; k < kMoves; ++k) {
+    const int64_t i = row0 + (k / PIECES) * groups;
+    const int w = w0 + (k % PIECES) * lanes;
+    if (i >= tokens.n || w >= words) continue;
     Vec<O, 8> o;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) o.v[c] = from_float<O>(t != kNoToken ? scale * ((float)((int)(q >> (4 * c) & 15) - 8) * s) : 0.0f);
+    for (int c = 0; c < 8; ++c) o.v[c] = from_float<O>(t[k / PIECES] != kNoToken ? scale * ((float)((int)(q[k] >> (4 * c) & 15) - 8) * s[k]) : 0.0f);
     O* at = out + i * out_stride + (int64_t)w * 8;
     if (ALIGNED) {
       *reinterpret_cast<Vec<O, 8>*>(at) = o;
@@ -120,9 +132,11 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // bytes, in one load (4, 8 or 16 bytes), and what the masks select of a word, columns p and p + 4, is a pair for the product.  The vectors are laid
 // out in shared memory to match, once per block.
 //
-// A warp has 16 rows at a time; where rows are long, `split` warps share 16 rows, a run of groups each.
+// A warp has 32 rows at a time, so that what it reads of the vectors serves two products; where there are few rows, `split` warps
+// share 32 rows, a run of groups each.  The scales of the groups in flight are read by the four threads of a row, one each.
 // ---------------------------------------------------------------------------
-constexpr int kTileRows = 16;
+constexpr int kTileRows = 32;
+constexpr int kScoreColumns = 256;                         // whose groups a warp has in flight
 
 struct Bf16Operand {
   using T = __nv_bfloat16;
@@ -132,9 +146,10 @@ struct Bf16Operand {
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x43084308u));     // 136
     return r;
   }
-  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  // d = a * b + c
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   }
 };
 struct F16Operand {
@@ -145,9 +160,9 @@ struct F16Operand {
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x64086408u));      // 1032
     return r;
   }
-  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   }
 };
 template <typename X> struct OperandOf { using type = Bf16Operand; static constexpr int parts = 1; };
@@ -171,32 +186,32 @@ __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y)
 
 template <int BYTES> struct Words { uint32_t w[BYTES / 4]; };
 template <int BYTES>
-__device__ __forceinline__ Words<BYTES> load_words(const uint8_t* at, bool there) {
-  Words<BYTES> r = {};
-  if (there) {
-    if constexpr (BYTES == 16) { const uint4 x = __ldg(reinterpret_cast<const uint4*>(at)); r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w; }
-    else if constexpr (BYTES == 8) { const uint2 x = __ldg(reinterpret_cast<const uint2*>(at)); r.w[0] = x.x; r.w[1] = x.y; }
-    else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
-  }
+__device__ __forceinline__ Words<BYTES> load_words(const uint8_t* at) {
+  Words<BYTES> r;
+  if constexpr (BYTES == 16) { const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at)); r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w; }
+  else if constexpr (BYTES == 8) { const uint2 x = __ldg(reinterpret_cast<const uint2*>(at)); r.w[0] = x.x; r.w[1] = x.y; }
+  else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
   return r;
 }
 
-// Columns of `columns` operands (vectors, or the parts of vectors) from x0 on.  Shared memory: [words of a row][columns][4 threads][4 pairs], then the sums of
-// the warps, [warps][16][8 * NT].
+// Columns of `columns` operands (vectors, or the parts of vectors) from x0 on.  Shared memory: [words of a row][columns][4 threads][4 pairs], 16 bytes of zeros,
+// then the sums of the warps, [warps][32][8 * NT].
 template <typename X, typename S, int GROUP, int NT, int THREADS>
-__global__ void __launch_bounds__(THREADS) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type, int64_t out_stride,
-                                                                 int split, int64_t tiles) {
+__global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
+                                                                                 int64_t out_stride, int split, int64_t tiles) {
   after_previous_kernel();
   using Op = typename OperandOf<X>::type;
   constexpr int PARTS = OperandOf<X>::parts;
   constexpr int BYTES = GROUP / 8, WORDS = BYTES / 4;       // of a row's group, a thread's quarter
-  constexpr int U = GROUP == 128 ? 4 : GROUP == 64 ? 4 : 8;  // groups in flight
+  constexpr int U = kScoreColumns / GROUP;                  // groups in flight
+  constexpr int SETS = kTileRows / 8;                       // rows of a thread: g, g + 8, ...
   constexpr int WARPS = THREADS / 32, N = 8 * NT;
   extern __shared__ uint4 shared[];
   const int columns = vectors * PARTS;
   const int row_words = p.groups * WORDS;                   // of a thread's quarter
-  uint4* operands = shared;                                 // [row_words][columns][4]
-  float* sums = reinterpret_cast<float*>(shared + (int64_t)row_words * columns * 4);
+  uint4* const operands = shared;                           // [row_words][columns][4]
+  uint4* const zeros = shared + row_words * columns * 4;
+  float* const sums = reinterpret_cast<float*>(zeros + 1);
 
   for (int i = threadIdx.x; i < row_words * columns * 4; i += THREADS) {
     const int t = i % 4, col = i / 4 % columns, w = i / 4 / columns;
@@ -211,105 +226,151 @@ __global__ void __launch_bounds__(THREADS) packed_scores_kernel(PackedView p, co
         e[2 * k + h] = c < p.cols ? part_of(from[c], col % PARTS) : from_float<typename Op::T>(0.0f);
       }
     }
-    operands[i] = *reinterpret_cast<const uint4*>(e);
+    memcpy(&operands[i], e, sizeof(uint4));
   }
+  if (threadIdx.x == 0) *zeros = make_uint4(0, 0, 0, 0);
   __syncthreads();
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const int share = warp % split, team = warp / split, teams = WARPS / split;
   const int per = (p.groups + split - 1) / split;
-  const int g0 = share * per, g1 = min(g0 + per, p.groups);
-  const int64_t row_bytes = (int64_t)((p.cols + 31) / 32) * 16;
+  const int g0 = min(share * per, p.groups), g1 = min(g0 + per, p.groups);
+  // A thread's bytes of a group.  Behind the row's end (the last group can be cut short) it reads the row's last bytes instead: the vectors are zero there.
+  const int row_bytes = (p.cols + 31) / 32 * 16, last_byte = row_bytes - BYTES;
+  const uint4* operand[NT];                                 // a column that there is none of: zeros
+  int operand_step[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const bool there = nt * 8 + g < columns;
+    operand[nt] = there ? operands + (nt * 8 + g) * 4 + t : zeros;
+    operand_step[nt] = there ? columns * 4 : 0;
+  }
+  const int full = min(g1, row_bytes / (GROUP / 2));        // groups whose bytes are all there
+  Words<BYTES> words[SETS][U];
+  constexpr int SCALES = (U + 3) / 4;
+  S scales[SETS][SCALES];                                   // of group t, t + 4 of those in flight
+  const auto load = [&](int64_t tile, int k0) {
+    const uint8_t* q[SETS];
+    const S* sc[SETS];
+#pragma unroll
+    for (int j = 0; j < SETS; ++j) {
+      const int64_t row = min(tile * kTileRows + g + 8 * j, p.rows - 1);
+      q[j] = p.q + row * p.q_stride + t * BYTES;
+      sc[j] = static_cast<const S*>(p.scales) + row * p.scale_stride;
+    }
+    if (k0 + U <= full) {
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) {
+        q[j] += k0 * (GROUP / 2);
+        sc[j] += k0 + (t & (U - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) words[j][u] = load_words<BYTES>(q[j] + u * (GROUP / 2));
+#pragma unroll
+        for (int u = 0; u < SCALES; ++u) scales[j][u] = sc[j][u * 4];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) words[j][u] = load_words<BYTES>(q[j] + min((k0 + u) * (GROUP / 2), last_byte - t * BYTES));
+#pragma unroll
+        for (int u = 0; u < SCALES; ++u) scales[j][u] = sc[j][min(k0 + u * 4 + (t & (U - 1)), p.groups - 1)];     // (behind the warp's share: read, not used)
+      }
+    }
+  };
 
-  for (int64_t first = (int64_t)blockIdx.x * teams; first < tiles; first += (int64_t)gridDim.x * teams) {
-    const int64_t row0 = (first + team) * kTileRows;
-    const int64_t ra = min(row0 + g, p.rows - 1), rb = min(row0 + g + 8, p.rows - 1);
-    const uint8_t *qa = p.q + ra * p.q_stride + t * BYTES, *qb = p.q + rb * p.q_stride + t * BYTES;
-    const S *sa = static_cast<const S*>(p.scales) + ra * p.scale_stride, *sb = static_cast<const S*>(p.scales) + rb * p.scale_stride;
-    float total[NT][4] = {};
-    if (row0 < p.rows) {
-      for (int k0 = g0; k0 < g1; k0 += U) {
-        Words<BYTES> wa[U], wb[U];
-        float fa[U], fb[U];
+  const int64_t step = (int64_t)gridDim.x * teams;
+  int64_t tile = (int64_t)blockIdx.x * teams + team;
+  if (tile < tiles) load(tile, g0);
+  for (; tile < tiles; tile += step) {
+    float total[SETS / 2][NT][4] = {};
+    for (int k0 = g0; k0 < g1; k0 += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int k = k0 + u;
-          const bool there = k < g1 && (int64_t)k * (GROUP / 2) + (t + 1) * BYTES <= row_bytes;
-          wa[u] = load_words<BYTES>(qa + k * (GROUP / 2), there);
-          wb[u] = load_words<BYTES>(qb + k * (GROUP / 2), there);
-          fa[u] = k < g1 ? to_float(sa[k]) : 0.0f;
-          fb[u] = k < g1 ? to_float(sb[k]) : 0.0f;
-        }
+      for (int u = 0; u < U; ++u) {
+        if (k0 + u >= g1) break;
+        float sum[SETS / 2][NT][4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int k = k0 + u;
-          if (k >= g1) break;
-          float sum[NT][4] = {};
+        for (int w = 0; w < WORDS; ++w) {
+          uint4 b[NT];
 #pragma unroll
-          for (int w = 0; w < WORDS; ++w) {
+          for (int nt = 0; nt < NT; ++nt) b[nt] = operand[nt][((k0 + u) * WORDS + w) * operand_step[nt]];
+#pragma unroll
+          for (int j = 0; j < SETS / 2; ++j) {
             uint32_t a[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              a[h][0] = Op::pair(wa[u].w[w] >> (8 * h));
-              a[h][1] = Op::pair(wb[u].w[w] >> (8 * h));
-              a[h][2] = Op::pair(wa[u].w[w] >> (8 * h + 4));
-              a[h][3] = Op::pair(wb[u].w[w] >> (8 * h + 4));
+              a[h][0] = Op::pair(words[2 * j][u].w[w] >> (8 * h));
+              a[h][1] = Op::pair(words[2 * j + 1][u].w[w] >> (8 * h));
+              a[h][2] = Op::pair(words[2 * j][u].w[w] >> (8 * h + 4));
+              a[h][3] = Op::pair(words[2 * j + 1][u].w[w] >> (8 * h + 4));
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              uint4 b = make_uint4(0, 0, 0, 0);
-              if (nt * 8 + g < columns) b = operands[((int64_t)(k * WORDS + w) * columns + nt * 8 + g) * 4 + t];
-              Op::mma(sum[nt], a[0], b.x, b.y);
-              Op::mma(sum[nt], a[1], b.z, b.w);
+              float(&d)[4] = sum[j][nt];
+              if (w == 0) Op::mma(d, a[0], b[nt].x, b[nt].y, 0.0f, 0.0f, 0.0f, 0.0f);
+              else Op::mma(d, a[0], b[nt].x, b[nt].y, d[0], d[1], d[2], d[3]);
+              Op::mma(d, a[1], b[nt].z, b[nt].w, d[0], d[1], d[2], d[3]);
             }
           }
+        }
+#pragma unroll
+        for (int j = 0; j < SETS; ++j) {
+          const float f = __shfl_sync(0xFFFFFFFFu, to_float(scales[j][u / 4]), (lane & ~3) | (u % 4));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            total[nt][0] += fa[u] * sum[nt][0];
-            total[nt][1] += fa[u] * sum[nt][1];
-            total[nt][2] += fb[u] * sum[nt][2];
-            total[nt][3] += fb[u] * sum[nt][3];
+            total[j / 2][nt][j % 2 * 2] += f * sum[j / 2][nt][j % 2 * 2];
+            total[j / 2][nt][j % 2 * 2 + 1] += f * sum[j / 2][nt][j % 2 * 2 + 1];
           }
         }
       }
+      // the next groups, or the next tile's first ones, on their way through the sums' end
+      const bool same = k0 + U < g1;
+      const int64_t next = same ? tile : tile + step;
+      if (next < tiles) load(next, same ? k0 + U : g0);
     }
-    float* mine = sums + warp * kTileRows * N;
+    float* const mine = sums + warp * kTileRows * N;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      mine[g * N + nt * 8 + 2 * t] = total[nt][0];
-      mine[g * N + nt * 8 + 2 * t + 1] = total[nt][1];
-      mine[(g + 8) * N + nt * 8 + 2 * t] = total[nt][2];
-      mine[(g + 8) * N + nt * 8 + 2 * t + 1] = total[nt][3];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < teams * kTileRows * vectors; i += THREADS) {
-      const int r = i % (teams * kTileRows), m = i / (teams * kTileRows);
-      const int64_t row = first * kTileRows + r;
-      if (row >= p.rows) continue;
-      float y = 0.0f;
-      for (int w = 0; w < split; ++w)
 #pragma unroll
-        for (int k = PARTS - 1; k >= 0; --k)                // (the small parts first)
-          y += sums[((r / kTileRows * split + w) * kTileRows + r % kTileRows) * N + m * PARTS + k];
-      store_as(out, out_type, m * out_stride + row, y);
+      for (int j = 0; j < SETS; ++j)
+        *reinterpret_cast<float2*>(mine + (g + 8 * j) * N + nt * 8 + 2 * t) = make_float2(total[j / 2][nt][j % 2 * 2], total[j / 2][nt][j % 2 * 2 + 1]);
     }
-    __syncthreads();
+    // the team's warps alone wait for one another
+    const auto wait = [&] {
+      if (split == 1) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(split * 32) : "memory");
+    };
+    wait();
+    const int64_t row0 = tile * kTileRows;
+    for (int i = share * 32 + lane; i < kTileRows * vectors; i += split * 32) {
+      const int r = i % kTileRows, m = i / kTileRows;
+      if (row0 + r >= p.rows) continue;
+      const float* from = sums + team * split * kTileRows * N + r * N + m * PARTS;
+      float y = 0.0f;
+      for (int w = 0; w < split; ++w) {
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k) y += from[w * kTileRows * N + k];      // (the small parts first)
+      }
+      store_as(out, out_type, m * out_stride + row0 + r, y);
+    }
+    wait();
   }
 }
 
 template <typename X, typename S, int GROUP, int NT, int THREADS>
 int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int vectors, void* out, int out_type, int64_t out_stride, cudaStream_t s) {
-  constexpr int WARPS = THREADS / 32, N = 8 * NT;
+  constexpr int WARPS = THREADS / 32, N = 8 * NT, U = kScoreColumns / GROUP;
   auto* kernel = packed_scores_kernel<X, S, GROUP, NT, THREADS>;
   const int columns = vectors * OperandOf<X>::parts;
-  const size_t shared = (size_t)p.groups * (GROUP / 32) * columns * 64 + (size_t)WARPS * kTileRows * N * 4;
-  int split = 1;
-  while (split < WARPS && p.groups >= split * 2 * 4) split *= 2;
+  const size_t shared = (size_t)p.groups * (GROUP / 32) * columns * 64 + 16 + (size_t)WARPS * kTileRows * N * 4;
   const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows;
+  // blocks that an SM holds, by registers and by shared memory (1 KB of it goes with each block)
+  const int blocks = (int)std::min<size_t>(2, (size_t)227 * 1024 / (shared + 1024));
+  // warps share a tile until each has had four tiles' worth of its own, as long as the share fills the loads in flight
+  int split = 1;
+  while (split < WARPS && tiles * split < 148ll * blocks * WARPS * 4 && p.groups >= split * 2 * U) split *= 2;
   const int teams = WARPS / split;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) return MONO_ERR_CUDA;
-  int blocks = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, THREADS, shared) != cudaSuccess || blocks < 1) return MONO_ERR_CUDA;
+  if (shared > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) return MONO_ERR_CUDA;
   const int64_t grid = std::min<int64_t>((tiles + teams - 1) / teams, 148ll * blocks);
   return launch_operator(kernel, dim3((unsigned)grid), THREADS, shared, s, p, x, x_stride, vectors, out, out_type, out_stride, split, tiles);
 }
@@ -369,16 +430,19 @@ int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int3
   const TokenList list{tokens, n_tokens, packed->rows, padding, token_type == MONO_I64};
   const int words = (p.cols + 7) / 8;
   int lanes = 1;
-  while (lanes < 32 && lanes < words) lanes *= 2;
-  const int64_t rows = kThreads / lanes;
-  const dim3 grid((unsigned)((n_tokens + rows - 1) / rows), (unsigned)((words + lanes - 1) / lanes));
+  const bool wide = words > 64;
+  while (wide ? lanes < kThreads && lanes * kMoves < words : lanes < words) lanes *= 2;
+  const int64_t rows = (int64_t)(kThreads / lanes) * (wide ? 1 : kMoves), columns = (int64_t)lanes * (wide ? kMoves : 1);
+  const dim3 grid((unsigned)((n_tokens + rows - 1) / rows), (unsigned)((words + columns - 1) / columns));
   return with_type(packed->scale_type, [&](auto s) {
     return with_type(out->type, [&](auto o) {
+      using S = decltype(s);
       using O = decltype(o);
       const auto launch = [&](auto* kernel) {
         return launch_operator(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), p, packed->group / 8, list, scale, static_cast<O*>(out->data), out->stride, lanes);
       };
-      return vector_of(*out) == 8 ? launch(packed_token_rows_kernel<decltype(s), O, true>) : launch(packed_token_rows_kernel<decltype(s), O, false>);
+      if (vector_of(*out) == 8) return wide ? launch(packed_token_rows_kernel<S, O, true, 1>) : launch(packed_token_rows_kernel<S, O, true, 4>);
+      return wide ? launch(packed_token_rows_kernel<S, O, false, 1>) : launch(packed_token_rows_kernel<S, O, false, 4>);
     });
   });
 }
