@@ -128,22 +128,38 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // per two weights.  Vectors in fp32 are three bf16 vectors whose sum they are exactly (8 bits of the significand each).  All products are exact, all sums in fp32.
 //
 // In a product of mma.m16n8k16 the columns are summed over, so any may stand in any place, as long as the vectors' are in the same.
-// So the rows are read as they lie: of a group of columns, thread t of the four that share a row has the t-th quarter of its
-// bytes, in one load (4, 8 or 16 bytes), and what the masks select of a word, columns p and p + 4, is a pair for the product.  The vectors are laid
-// out in shared memory to match, once per block.
+// So thread t of the four that share a row takes the t-th quarter of a group's bytes as they lie, and what the masks select of a word, columns p
+// and p + 4, is a pair for the product.  The vectors are laid out in shared memory to match, once per block.
 //
-// A warp has 32 rows at a time, so that what it reads of the vectors serves two products; where there are few rows, `split` warps
-// share 32 rows, a run of groups each.  The scales of the groups in flight are read by the four threads of a row, one each.
+// A warp has 32 rows at a time, so that what it reads of the vectors serves two products, and moves 128 columns of them (64 bytes of each) to
+// shared memory of its own, kStages - 1 moves ahead of the products.  Read straight into registers, the eight rows of a load are eight
+// short pieces, and a third more time went with them (8 vectors, 131072 rows of 4096: 84 us).  Where there are few rows, `split` warps share
+// 32 rows, a run of columns each.  Scales are read ahead by the four threads of a row, one each.
 // ---------------------------------------------------------------------------
 constexpr int kTileRows = 32;
-constexpr int kScoreColumns = 256;                         // whose groups a warp has in flight
+constexpr int kBlockColumns = 128, kBlockBytes = kBlockColumns / 2;
+constexpr int kMostWarps = 16;
+constexpr int kStages = 4;
+constexpr int kStageBytes = kTileRows * kBlockBytes;
+
+// (w & mask) | bits in one instruction: with both constants written out the compiler made two
+__device__ __forceinline__ uint32_t place(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+__device__ __forceinline__ uint32_t kept(uint32_t constant) {
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(constant));
+  return r;
+}
 
 struct Bf16Operand {
   using T = __nv_bfloat16;
-  static __device__ __forceinline__ uint32_t pair(uint32_t w) {            // columns in bits 0..3 and 16..19
-    const uint32_t biased = (w & 0x000F000Fu) | 0x43004300u;               // 128 + q
+  static constexpr uint32_t kBits = 0x43004300u;                           // 128
+  static __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t mask, uint32_t bits) {      // columns in bits 0..3 and 16..19
     uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x43084308u));     // 136
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(place(w, mask, bits)), "r"(0x43084308u));      // 136
     return r;
   }
   // d = a * b + c
@@ -154,10 +170,10 @@ struct Bf16Operand {
 };
 struct F16Operand {
   using T = __half;
-  static __device__ __forceinline__ uint32_t pair(uint32_t w) {
-    const uint32_t biased = (w & 0x000F000Fu) | 0x64006400u;               // 1024 + q
+  static constexpr uint32_t kBits = 0x64006400u;                           // 1024
+  static __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t mask, uint32_t bits) {
     uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x64086408u));      // 1032
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(place(w, mask, bits)), "r"(0x64086408u));       // 1032
     return r;
   }
   static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
@@ -184,38 +200,66 @@ __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y)
   else static_cast<__half*>(to)[i] = from_float<__half>(y);
 }
 
-template <int BYTES> struct Words { uint32_t w[BYTES / 4]; };
-template <int BYTES>
-__device__ __forceinline__ Words<BYTES> load_words(const uint8_t* at) {
-  Words<BYTES> r;
-  if constexpr (BYTES == 16) { const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at)); r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w; }
-  else if constexpr (BYTES == 8) { const uint2 x = __ldg(reinterpret_cast<const uint2*>(at)); r.w[0] = x.x; r.w[1] = x.y; }
-  else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
-  return r;
-}
+template <int BYTES> struct alignas(BYTES) Words { uint32_t w[BYTES / 4]; };
 
-// Columns of `columns` operands (vectors, or the parts of vectors) from x0 on.  Shared memory: [words of a row][columns][4 threads][4 pairs], 16 bytes of zeros,
-// then the sums of the warps, [warps][32][8 * NT].
-template <typename X, typename S, int GROUP, int NT, int THREADS>
-__global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
-                                                                                 int64_t out_stride, int split, int64_t tiles) {
+// Shared memory: the warps' stages, [warps][kStages][32][64 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; 16 bytes of zeros;
+// the sums of the warps, [warps][32][8 * NT].  `columns` operands: vectors, or the parts of vectors.
+template <typename X, typename S, int GROUP, int NT>
+__global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
+                                                               int64_t out_stride, int split, int64_t tiles) {
   after_previous_kernel();
   using Op = typename OperandOf<X>::type;
   constexpr int PARTS = OperandOf<X>::parts;
   constexpr int BYTES = GROUP / 8, WORDS = BYTES / 4;       // of a row's group, a thread's quarter
-  constexpr int U = kScoreColumns / GROUP;                  // groups in flight
+  constexpr int U = kBlockColumns / GROUP;                  // groups of a stage
   constexpr int SETS = kTileRows / 8;                       // rows of a thread: g, g + 8, ...
-  constexpr int WARPS = THREADS / 32, N = 8 * NT;
-  extern __shared__ uint4 shared[];
-  const int columns = vectors * PARTS;
+  constexpr int N = 8 * NT;
+  extern __shared__ __align__(128) uint4 shared[];
+  const int warps = blockDim.x / 32, columns = vectors * PARTS;
   const int row_words = p.groups * WORDS;                   // of a thread's quarter
-  uint4* const operands = shared;                           // [row_words][columns][4]
-  uint4* const zeros = shared + row_words * columns * 4;
+  uint4* const operands = shared + warps * kStages * (kStageBytes / 16);
+  uint4* const zeros = operands + row_words * columns * 4;
   float* const sums = reinterpret_cast<float*>(zeros + 1);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+  const int share = warp % split, team = warp / split, teams = warps / split;
+  const int blocks = (p.groups + U - 1) / U, per = (blocks + split - 1) / split;
+  const int k0 = min(share * per, blocks), k1 = min(k0 + per, blocks);      // this warp's blocks of columns
+  const int row_bytes = (p.cols + 31) / 32 * 16;
+  const int64_t step = (int64_t)gridDim.x * teams, tile0 = (int64_t)blockIdx.x * teams + team;
 
-  for (int i = threadIdx.x; i < row_words * columns * 4; i += THREADS) {
-    const int t = i % 4, col = i / 4 % columns, w = i / 4 / columns;
-    const int c0 = (w / WORDS) * GROUP + t * (GROUP / 4) + w % WORDS * 8;
+  // A stage: the lane has 16 bytes of rows lane / 4, lane / 4 + 8, ...  Where they go is turned by the row, so that the threads that read
+  // a group together find their bytes in different banks.
+  uint4* const stages = shared + warp * kStages * (kStageBytes / 16);
+  const auto turned = [](int row, int piece) { return row * 4 + (piece ^ (GROUP == 128 ? 0 : GROUP == 64 ? row & 2 : row >> 1 & 3)); };
+  int64_t fill_tile = tile0;
+  int fill_k = k0, fill_stage = 0;
+  const uint8_t* fill_from[kTileRows / 8];                  // the lane's bytes of its rows
+  const uint32_t fill_to = (uint32_t)__cvta_generic_to_shared(stages) + turned(g, t) * 16;
+  const auto fill = [&] {
+    if (fill_tile < tiles) {
+      if (fill_k == k0) {
+#pragma unroll
+        for (int i = 0; i < kTileRows / 8; ++i) fill_from[i] = p.q + min(fill_tile * kTileRows + g + 8 * i, p.rows - 1) * p.q_stride + (k0 * kBlockBytes + t * 16);
+      }
+      if (fill_k * kBlockBytes + t * 16 < row_bytes) {      // (behind the row's end the vectors are zero, whatever the stage holds)
+        const uint32_t to = fill_to + fill_stage * kStageBytes;
+#pragma unroll
+        for (int i = 0; i < kTileRows / 8; ++i) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 8 * kBlockBytes), "l"(fill_from[i]) : "memory");
+          fill_from[i] += kBlockBytes;
+        }
+      }
+      if (++fill_k >= k1) { fill_k = k0; fill_tile += step; }
+    }
+    fill_stage = (fill_stage + 1) % kStages;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int s = 0; s < kStages - 1; ++s) fill();
+
+  for (int i = threadIdx.x; i < row_words * columns * 4; i += blockDim.x) {
+    const int part = i % 4, col = i / 4 % columns, w = i / 4 / columns;
+    const int c0 = (w / WORDS) * GROUP + part * (GROUP / 4) + w % WORDS * 8;
     const X* from = x + (col / PARTS) * x_stride;
     typename Op::T e[8];
 #pragma unroll
@@ -229,80 +273,73 @@ __global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p,
     memcpy(&operands[i], e, sizeof(uint4));
   }
   if (threadIdx.x == 0) *zeros = make_uint4(0, 0, 0, 0);
-  __syncthreads();
 
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-  const int share = warp % split, team = warp / split, teams = WARPS / split;
-  const int per = (p.groups + split - 1) / split;
-  const int g0 = min(share * per, p.groups), g1 = min(g0 + per, p.groups);
-  // A thread's bytes of a group.  Behind the row's end (the last group can be cut short) it reads the row's last bytes instead: the vectors are zero there.
-  const int row_bytes = (p.cols + 31) / 32 * 16, last_byte = row_bytes - BYTES;
-  const uint4* operand[NT];                                 // a column that there is none of: zeros
+  S scales[SETS];                                           // of group t (modulo U) of the next block of columns
+  const S* scale_row[SETS];
+  const auto load_scales = [&](int64_t tile, int k) {
+    if (k == k0) {
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) scale_row[j] = static_cast<const S*>(p.scales) + min(tile * kTileRows + g + 8 * j, p.rows - 1) * p.scale_stride;
+    }
+    const int at = min(k * U + (t & (U - 1)), p.groups - 1);
+#pragma unroll
+    for (int j = 0; j < SETS; ++j) scales[j] = scale_row[j][at];
+  };
+  if (tile0 < tiles) load_scales(tile0, k0);
+  int operand[NT];                                          // in shared[]; of a column that there is none of: zeros
   int operand_step[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const bool there = nt * 8 + g < columns;
-    operand[nt] = there ? operands + (nt * 8 + g) * 4 + t : zeros;
+    operand[nt] = (int)(there ? operands + (nt * 8 + g) * 4 + t - shared : zeros - shared) + (there ? k0 * U * WORDS * columns * 4 : 0);
     operand_step[nt] = there ? columns * 4 : 0;
   }
-  const int full = min(g1, row_bytes / (GROUP / 2));        // groups whose bytes are all there
-  Words<BYTES> words[SETS][U];
-  constexpr int SCALES = (U + 3) / 4;
-  S scales[SETS][SCALES];                                   // of group t, t + 4 of those in flight
-  const auto load = [&](int64_t tile, int k0) {
-    const uint8_t* q[SETS];
-    const S* sc[SETS];
-#pragma unroll
-    for (int j = 0; j < SETS; ++j) {
-      const int64_t row = min(tile * kTileRows + g + 8 * j, p.rows - 1);
-      q[j] = p.q + row * p.q_stride + t * BYTES;
-      sc[j] = static_cast<const S*>(p.scales) + row * p.scale_stride;
-    }
-    if (k0 + U <= full) {
-#pragma unroll
-      for (int j = 0; j < SETS; ++j) {
-        q[j] += k0 * (GROUP / 2);
-        sc[j] += k0 + (t & (U - 1));
-#pragma unroll
-        for (int u = 0; u < U; ++u) words[j][u] = load_words<BYTES>(q[j] + u * (GROUP / 2));
-#pragma unroll
-        for (int u = 0; u < SCALES; ++u) scales[j][u] = sc[j][u * 4];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < SETS; ++j) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) words[j][u] = load_words<BYTES>(q[j] + min((k0 + u) * (GROUP / 2), last_byte - t * BYTES));
-#pragma unroll
-        for (int u = 0; u < SCALES; ++u) scales[j][u] = sc[j][min(k0 + u * 4 + (t & (U - 1)), p.groups - 1)];     // (behind the warp's share: read, not used)
-      }
-    }
-  };
+  const uint32_t mask = kept(0x000F000Fu), bits = kept(Op::kBits);
+  const int stage_bytes = warp * kStages * kStageBytes;     // where the warp's stages begin in shared[]
+  int stage = 0;
+  __syncthreads();
 
-  const int64_t step = (int64_t)gridDim.x * teams;
-  int64_t tile = (int64_t)blockIdx.x * teams + team;
-  if (tile < tiles) load(tile, g0);
-  for (; tile < tiles; tile += step) {
+  for (int64_t tile = tile0; tile < tiles; tile += step) {
     float total[SETS / 2][NT][4] = {};
-    for (int k0 = g0; k0 < g1; k0 += U) {
+    int at_operand[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) at_operand[nt] = operand[nt];
+    for (int k = k0; k < k1; ++k) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      __syncwarp();                                         // the stage is there for the warp, and it is done with the one that is filled now
+      fill();
+      S own[SETS];
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) own[j] = scales[j];
+      const bool same = k + 1 < k1;
+      if (same || tile + step < tiles) load_scales(same ? tile : tile + step, same ? k + 1 : k0);
+      const int from = stage_bytes + stage * kStageBytes;
+      stage = (stage + 1) % kStages;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (k0 + u >= g1) break;
+        if (k * U + u >= p.groups) break;
+        Words<BYTES> words[SETS];
+        const int at = (u * 4 + t) * BYTES;                 // in the row's bytes
+#pragma unroll
+        for (int j = 0; j < SETS; ++j) words[j] = *reinterpret_cast<const Words<BYTES>*>(reinterpret_cast<const char*>(shared) + (from + turned(g + 8 * j, at / 16) * 16 + at % 16));
         float sum[SETS / 2][NT][4];
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
           uint4 b[NT];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) b[nt] = operand[nt][((k0 + u) * WORDS + w) * operand_step[nt]];
+          for (int nt = 0; nt < NT; ++nt) {
+            b[nt] = shared[at_operand[nt]];
+            at_operand[nt] += operand_step[nt];
+          }
 #pragma unroll
           for (int j = 0; j < SETS / 2; ++j) {
             uint32_t a[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              a[h][0] = Op::pair(words[2 * j][u].w[w] >> (8 * h));
-              a[h][1] = Op::pair(words[2 * j + 1][u].w[w] >> (8 * h));
-              a[h][2] = Op::pair(words[2 * j][u].w[w] >> (8 * h + 4));
-              a[h][3] = Op::pair(words[2 * j + 1][u].w[w] >> (8 * h + 4));
+              a[h][0] = Op::pair(words[2 * j].w[w] >> (8 * h), mask, bits);
+              a[h][1] = Op::pair(words[2 * j + 1].w[w] >> (8 * h), mask, bits);
+              a[h][2] = Op::pair(words[2 * j].w[w] >> (8 * h + 4), mask, bits);
+              a[h][3] = Op::pair(words[2 * j + 1].w[w] >> (8 * h + 4), mask, bits);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -315,7 +352,7 @@ __global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p,
         }
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-          const float f = __shfl_sync(0xFFFFFFFFu, to_float(scales[j][u / 4]), (lane & ~3) | (u % 4));
+          const float f = U == 1 ? to_float(own[j]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j]), (lane & ~3) | u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             total[j / 2][nt][j % 2 * 2] += f * sum[j / 2][nt][j % 2 * 2];
@@ -323,10 +360,6 @@ __global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p,
           }
         }
       }
-      // the next groups, or the next tile's first ones, on their way through the sums' end
-      const bool same = k0 + U < g1;
-      const int64_t next = same ? tile : tile + step;
-      if (next < tiles) load(next, same ? k0 + U : g0);
     }
     float* const mine = sums + warp * kTileRows * N;
 #pragma unroll
@@ -355,39 +388,47 @@ __global__ void __launch_bounds__(THREADS, 2) packed_scores_kernel(PackedView p,
     }
     wait();
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <typename X, typename S, int GROUP, int NT, int THREADS>
+// Of a block with so many warps, for so many operand vectors.
+inline size_t scores_shared(int warps, int64_t groups, int group, int columns, int nt) {
+  return (size_t)warps * kStages * kStageBytes + (size_t)groups * (group / 32) * columns * 64 + 16 + (size_t)warps * kTileRows * 8 * nt * 4;
+}
+constexpr size_t kMostShared = 227 * 1024;
+
+template <typename X, typename S, int GROUP, int NT>
 int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int vectors, void* out, int out_type, int64_t out_stride, cudaStream_t s) {
-  constexpr int WARPS = THREADS / 32, N = 8 * NT, U = kScoreColumns / GROUP;
-  auto* kernel = packed_scores_kernel<X, S, GROUP, NT, THREADS>;
+  auto* kernel = packed_scores_kernel<X, S, GROUP, NT>;
   const int columns = vectors * OperandOf<X>::parts;
-  const size_t shared = (size_t)p.groups * (GROUP / 32) * columns * 64 + 16 + (size_t)WARPS * kTileRows * N * 4;
-  const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows;
-  // blocks that an SM holds, by registers and by shared memory (1 KB of it goes with each block)
-  const int blocks = (int)std::min<size_t>(2, (size_t)227 * 1024 / (shared + 1024));
-  // warps share a tile until each has had four tiles' worth of its own, as long as the share fills the loads in flight
+  const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows, blocks = ((int64_t)p.groups * GROUP + kBlockColumns - 1) / kBlockColumns;
+  int warps = kMostWarps;
+  while (scores_shared(warps, p.groups, GROUP, columns, NT) > kMostShared) warps /= 2;
+  // warps share a tile until each has had four tiles' worth of its own, as long as there are columns for each
   int split = 1;
-  while (split < WARPS && tiles * split < 148ll * blocks * WARPS * 4 && p.groups >= split * 2 * U) split *= 2;
-  const int teams = WARPS / split;
-  if (shared > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared) != cudaSuccess) return MONO_ERR_CUDA;
-  const int64_t grid = std::min<int64_t>((tiles + teams - 1) / teams, 148ll * blocks);
-  return launch_operator(kernel, dim3((unsigned)grid), THREADS, shared, s, p, x, x_stride, vectors, out, out_type, out_stride, split, tiles);
+  while (split < warps && split < 8 && tiles * split < 148ll * warps * 4 && blocks >= split * 2) split *= 2;
+  // small blocks where there is little for all SMs
+  while (warps > split && warps > 2 && tiles * split <= 148ll * warps / 2) warps /= 2;
+  const size_t shared = scores_shared(warps, p.groups, GROUP, columns, NT);
+  const int teams = warps / split;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared) != cudaSuccess) return MONO_ERR_CUDA;
+  const int64_t grid = std::min<int64_t>((tiles + teams - 1) / teams, 148);
+  return launch_operator(kernel, dim3((unsigned)grid), warps * 32, shared, s, p, x, x_stride, vectors, out, out_type, out_stride, split, tiles);
 }
 
 template <typename X, typename S, int GROUP>
 int launch_scores(const mono_packed_t& packed, const mono_matrix_t& x, const mono_matrix_t& out, cudaStream_t s) {
   constexpr int PARTS = OperandOf<X>::parts;
   const PackedView p = view(packed);
-  const int64_t operand_bytes = (int64_t)p.groups * GROUP * 2;                    // of one operand vector in shared memory
-  // vectors of a launch: up to 16 operands, and no more than shared memory has room for
-  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(16 / PARTS, (200 * 1024) / (operand_bytes * PARTS)));
+  // vectors of a launch: up to 16 operands, and no more than shared memory has room for beside the stages of two warps
+  int most = 16 / PARTS;
+  while (most > 1 && scores_shared(2, p.groups, GROUP, most * PARTS, 2) > kMostShared) --most;
   for (int64_t m = 0; m < x.rows; m += most) {
     const int vectors = (int)std::min<int64_t>(most, x.rows - m);
     const X* from = static_cast<const X*>(x.data) + m * x.stride;
     char* to = static_cast<char*>(out.data) + m * out.stride * element_size(out.type);
-    const int rc = vectors * PARTS <= 8 ? launch_scores_tile<X, S, GROUP, 1, kThreads>(p, from, x.stride, vectors, to, out.type, out.stride, s)
-                                        : launch_scores_tile<X, S, GROUP, 2, kThreads>(p, from, x.stride, vectors, to, out.type, out.stride, s);
+    const int rc = vectors * PARTS <= 8 ? launch_scores_tile<X, S, GROUP, 1>(p, from, x.stride, vectors, to, out.type, out.stride, s)
+                                        : launch_scores_tile<X, S, GROUP, 2>(p, from, x.stride, vectors, to, out.type, out.stride, s);
     if (rc != MONO_OK) return rc;
   }
   return MONO_OK;
