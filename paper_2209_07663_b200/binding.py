@@ -604,6 +604,21 @@ class MonoTable:
             out["w"], out["acc"] = w[:m].cpu().numpy()[order], acc[:m].cpu().numpy()[order]
         return out
 
+    def export_packed(self, group: int = 64, scale_dtype=None):
+        """The rows in 4 bits for a serving process: (int64 tensor of the IDs that own rows, their PackedRows), sorted by
+        the IDs' bits as signed numbers, both on the device."""
+        torch = self._torch
+        from .tokens import PackedRows
+        n = int(self.status()["n_tracked"]) + 8
+        ids = torch.empty(n, dtype=torch.int64, device="cuda")
+        resident = torch.empty(n, dtype=torch.uint8, device="cuda")
+        w = torch.empty((n, self.dim), dtype=torch.float32, device="cuda")
+        count, seen = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int64, device="cuda")
+        m = mono_export(self.handle, ids, count, seen, resident, w, None, n)
+        owns = resident[:m].nonzero()[:, 0]
+        ids, order = torch.sort(ids[:m][owns])
+        return ids, PackedRows.pack(w[owns[order]], group, scale_dtype or torch.float16)
+
     def rehash(self, new_key_cells: int = 0, new_seed: int = 0):
         mono_rehash(self.handle, new_key_cells, new_seed)
 
