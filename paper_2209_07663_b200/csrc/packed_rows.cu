@@ -122,10 +122,14 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // ---------------------------------------------------------------------------
 // Scores.  out[m, v] = sum over groups g of s[v, g] * (sum over c in g of x[m, c] * (q[v, c] - 8)).
 //
-// The bytes of q bound it (half a byte for 2 * m operations), so a weight has to become an operand in few instructions: the tensor
-// cores' 16-bit products take 16 rows and 8 vectors at once.  4 bits placed in the low mantissa of 2^7 (bf16) or 2^10 (fp16)
-// are 128 + q or 1024 + q; less 136 or 1032, exact in either type, they are q - 8: with the shift, one and a half instructions
-// per two weights.  Vectors in fp32 are three bf16 vectors whose sum they are exactly (8 bits of the significand each).  All products are exact, all sums in fp32.
+// The bytes of q bound it (half a byte for 2 * m operations), if a weight becomes an operand in few enough instructions: the tensor
+// cores' 16-bit products take 16 rows and 8 vectors at once.  As the bits of an fp16, 4 bits in the lowest places are q * 2^-24 and in
+// the next ones 16 * q * 2^-24, subnormal and exact; times 2^14 or 2^10, less 8 * 2^-10, they are (q - 8) * 2^-10: an AND and
+// a multiply-add for two weights, and a shift for each eight.  (Left subnormal, with the 8 taken off the sums, they took 71 us instead of
+// 74 for 8 vectors against 131072 rows of 4096 columns, and the sums lost three bits.)
+// Vectors become fp16 operands that lose nothing that fp32 sums would keep: those of a group are multiplied by the power of two that takes
+// the largest of them to 2^14 .. 2^15, so that only what is below 2^-36 of it is rounded at all, and fp32 vectors are three operands
+// whose sum they are.  All products are exact, all sums in fp32.
 //
 // In a product of mma.m16n8k16 the columns are summed over, so any may stand in any place, as long as the vectors' are in the same.
 // So thread t of the four that share a row takes the t-th quarter of a group's bytes as they lie, and what the masks select of a word, columns p
@@ -142,10 +146,18 @@ constexpr int kMostWarps = 16;
 constexpr int kStages = 4;
 constexpr int kStageBytes = kTileRows * kBlockBytes;
 
-// (w & mask) | bits in one instruction: with both constants written out the compiler made two
-__device__ __forceinline__ uint32_t place(uint32_t w, uint32_t mask, uint32_t bits) {
+template <typename X> struct PartsOf { static constexpr int value = 1; };
+template <> struct PartsOf<float> { static constexpr int value = 3; };
+
+// d = a * b + c
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+// (q - 8) * 2^-10 of two weights, of q * 2^-24 (by 2^14) or 16 * q * 2^-24 (by 2^10)
+__device__ __forceinline__ uint32_t weights(uint32_t q, uint32_t by) {
   uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(q), "r"(by), "r"(0xA000A000u));
   return r;
 }
 __device__ __forceinline__ uint32_t kept(uint32_t constant) {
@@ -153,46 +165,7 @@ __device__ __forceinline__ uint32_t kept(uint32_t constant) {
   asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(constant));
   return r;
 }
-
-struct Bf16Operand {
-  using T = __nv_bfloat16;
-  static constexpr uint32_t kBits = 0x43004300u;                           // 128
-  static __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t mask, uint32_t bits) {      // columns in bits 0..3 and 16..19
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(place(w, mask, bits)), "r"(0x43084308u));      // 136
-    return r;
-  }
-  // d = a * b + c
-  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-  }
-};
-struct F16Operand {
-  using T = __half;
-  static constexpr uint32_t kBits = 0x64006400u;                           // 1024
-  static __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t mask, uint32_t bits) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(place(w, mask, bits)), "r"(0x64086408u));       // 1032
-    return r;
-  }
-  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-  }
-};
-template <typename X> struct OperandOf { using type = Bf16Operand; static constexpr int parts = 1; };
-template <> struct OperandOf<__half> { using type = F16Operand; static constexpr int parts = 1; };
-template <> struct OperandOf<float> { using type = Bf16Operand; static constexpr int parts = 3; };
-
-// part `k` of x as an operand
-__device__ __forceinline__ __nv_bfloat16 part_of(__nv_bfloat16 x, int) { return x; }
-__device__ __forceinline__ __half part_of(__half x, int) { return x; }
-__device__ __forceinline__ __nv_bfloat16 part_of(float x, int k) {
-  if (!(fabsf(x) <= 3.402823466e38f)) return __float2bfloat16_rn(k == 0 ? x : 0.0f);
-  for (; k > 0; --k) x -= __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);     // cut, not rounded: what is left is exact
-  return __float2bfloat16_rn(__uint_as_float(__float_as_uint(x) & 0xFFFF0000u));
-}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127
 
 __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y) {
   if (type == MONO_F32) static_cast<float*>(to)[i] = y;
@@ -202,14 +175,14 @@ __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y)
 
 template <int BYTES> struct alignas(BYTES) Words { uint32_t w[BYTES / 4]; };
 
-// Shared memory: the warps' stages, [warps][kStages][32][64 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; 16 bytes of zeros;
-// the sums of the warps, [warps][32][8 * NT].  `columns` operands: vectors, or the parts of vectors.
+// Shared memory: the warps' stages, [warps][kStages][32][64 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; of each group, [4 * NT]
+// pairs of columns: the powers of two; the sums of the warps, [warps][32][8 * NT].  `columns` operands:
+// vectors, or the parts of vectors.
 template <typename X, typename S, int GROUP, int NT>
 __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
                                                                int64_t out_stride, int split, int64_t tiles) {
   after_previous_kernel();
-  using Op = typename OperandOf<X>::type;
-  constexpr int PARTS = OperandOf<X>::parts;
+  constexpr int PARTS = PartsOf<X>::value;
   constexpr int BYTES = GROUP / 8, WORDS = BYTES / 4;       // of a row's group, a thread's quarter
   constexpr int U = kBlockColumns / GROUP;                  // groups of a stage
   constexpr int SETS = kTileRows / 8;                       // rows of a thread: g, g + 8, ...
@@ -218,8 +191,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
   const int warps = blockDim.x / 32, columns = vectors * PARTS;
   const int row_words = p.groups * WORDS;                   // of a thread's quarter
   uint4* const operands = shared + warps * kStages * (kStageBytes / 16);
-  uint4* const zeros = operands + row_words * columns * 4;
-  float* const sums = reinterpret_cast<float*>(zeros + 1);
+  float2* const groups = reinterpret_cast<float2*>(operands + row_words * columns * 4);
+  float* const sums = reinterpret_cast<float*>(groups + p.groups * 4 * NT);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const int share = warp % split, team = warp / split, teams = warps / split;
   const int blocks = (p.groups + U - 1) / U, per = (blocks + split - 1) / split;
@@ -257,22 +230,53 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
 #pragma unroll 1
   for (int s = 0; s < kStages - 1; ++s) fill();
 
-  for (int i = threadIdx.x; i < row_words * columns * 4; i += blockDim.x) {
-    const int part = i % 4, col = i / 4 % columns, w = i / 4 / columns;
-    const int c0 = (w / WORDS) * GROUP + part * (GROUP / 4) + w % WORDS * 8;
-    const X* from = x + (col / PARTS) * x_stride;
-    typename Op::T e[8];
+  // The vectors as operands: a thread has 8 neighbouring columns, GROUP / 8 threads a group.
+  for (int i = threadIdx.x; i < p.groups * 4 * NT; i += blockDim.x) groups[i] = make_float2(0.0f, 0.0f);
+  __syncthreads();
+  {
+    const int eights = p.groups * (GROUP / 8), items = eights * vectors, rounds = (items + blockDim.x - 1) / blockDim.x;
+    for (int round = 0; round < rounds; ++round) {
+      const int i = round * blockDim.x + threadIdx.x, m = min(i / eights, vectors - 1), c0 = (i - m * eights) * 8;
+      const X* from = x + m * x_stride;
+      float v[8];
+      uint32_t most = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 8; ++k) {
+        v[k] = i < items && c0 + k < p.cols ? to_float(from[c0 + k]) : 0.0f;
+        const uint32_t size = __float_as_uint(v[k]) & 0x7FFFFFFFu;
+        if (size < 0x7F800000u) most = max(most, size);
+      }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = c0 + k + 4 * h;
-        e[2 * k + h] = c < p.cols ? part_of(from[c], col % PARTS) : from_float<typename Op::T>(0.0f);
+      for (int s = GROUP / 16; s > 0; s /= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, s));
+      const int e = max((int)(most >> 23), 1) - 127;         // of the largest; a subnormal's is that of the smallest normal number
+      const float up0 = power_of_two((14 - e) / 2), up1 = power_of_two(14 - e - (14 - e) / 2);
+      __half part[PARTS][8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        float left = v[k] * up0 * up1;
+#pragma unroll
+        for (int j = 0; j < PARTS; ++j) {
+          // (cut, so that what is left has the same sign and fewer bits; of what is not finite nothing is left)
+          part[j][k] = j + 1 < PARTS ? __float2half_rz(left) : __float2half_rn(left);
+          left = fabsf(left) < 65536.0f ? left - __half2float(part[j][k]) : 0.0f;
+          if (PARTS > 1 && j == 0 && !(fabsf(v[k]) <= 3.402823466e38f)) part[j][k] = __float2half_rn(v[k]);
+        }
+      }
+      if (i >= items) continue;
+      const int group = c0 / GROUP, in = c0 % GROUP, word = group * WORDS + in % (GROUP / 4) / 8;
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int col = m * PARTS + j;
+        __half e8[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e8[2 * k] = part[j][k], e8[2 * k + 1] = part[j][k + 4];
+        memcpy(&operands[(word * columns + col) * 4 + in / (GROUP / 4)], e8, sizeof(uint4));
+        if (in == 0) {
+          reinterpret_cast<float*>(&groups[group * 4 * NT + col / 2])[col % 2] = power_of_two(e);
+        }
       }
     }
-    memcpy(&operands[i], e, sizeof(uint4));
   }
-  if (threadIdx.x == 0) *zeros = make_uint4(0, 0, 0, 0);
 
   S scales[SETS];                                           // of group t (modulo U) of the next block of columns
   const S* scale_row[SETS];
@@ -286,15 +290,11 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
     for (int j = 0; j < SETS; ++j) scales[j] = scale_row[j][at];
   };
   if (tile0 < tiles) load_scales(tile0, k0);
-  int operand[NT];                                          // in shared[]; of a column that there is none of: zeros
-  int operand_step[NT];
+  int operand[NT];                                          // in shared[]; for a column that there is none of another one's: its sums are not written
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const bool there = nt * 8 + g < columns;
-    operand[nt] = (int)(there ? operands + (nt * 8 + g) * 4 + t - shared : zeros - shared) + (there ? k0 * U * WORDS * columns * 4 : 0);
-    operand_step[nt] = there ? columns * 4 : 0;
-  }
-  const uint32_t mask = kept(0x000F000Fu), bits = kept(Op::kBits);
+  for (int nt = 0; nt < NT; ++nt) operand[nt] = (int)(operands - shared) + (k0 * U * WORDS * columns + min(nt * 8 + g, columns - 1)) * 4 + t;
+  const int operand_step = columns * 4;
+  const uint32_t by14 = kept(0x74007400u), by10 = kept(0x64006400u);      // 2^14, 2^10
   const int stage_bytes = warp * kStages * kStageBytes;     // where the warp's stages begin in shared[]
   int stage = 0;
   __syncthreads();
@@ -322,41 +322,46 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
         const int at = (u * 4 + t) * BYTES;                 // in the row's bytes
 #pragma unroll
         for (int j = 0; j < SETS; ++j) words[j] = *reinterpret_cast<const Words<BYTES>*>(reinterpret_cast<const char*>(shared) + (from + turned(g + 8 * j, at / 16) * 16 + at % 16));
+        float2 of_group[NT];                                // of columns 2 * t and the one behind it
         float sum[SETS / 2][NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) of_group[nt] = groups[(k * U + u) * 4 * NT + nt * 4 + t];
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
           uint4 b[NT];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             b[nt] = shared[at_operand[nt]];
-            at_operand[nt] += operand_step[nt];
+            at_operand[nt] += operand_step;
           }
 #pragma unroll
           for (int j = 0; j < SETS / 2; ++j) {
             uint32_t a[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              a[h][0] = Op::pair(words[2 * j].w[w] >> (8 * h), mask, bits);
-              a[h][1] = Op::pair(words[2 * j + 1].w[w] >> (8 * h), mask, bits);
-              a[h][2] = Op::pair(words[2 * j].w[w] >> (8 * h + 4), mask, bits);
-              a[h][3] = Op::pair(words[2 * j + 1].w[w] >> (8 * h + 4), mask, bits);
+              const uint32_t w0 = words[2 * j].w[w] >> (8 * h), w1 = words[2 * j + 1].w[w] >> (8 * h);
+              a[h][0] = weights(w0 & 0x000F000Fu, by14);
+              a[h][1] = weights(w1 & 0x000F000Fu, by14);
+              a[h][2] = weights(w0 & 0x00F000F0u, by10);
+              a[h][3] = weights(w1 & 0x00F000F0u, by10);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float(&d)[4] = sum[j][nt];
-              if (w == 0) Op::mma(d, a[0], b[nt].x, b[nt].y, 0.0f, 0.0f, 0.0f, 0.0f);
-              else Op::mma(d, a[0], b[nt].x, b[nt].y, d[0], d[1], d[2], d[3]);
-              Op::mma(d, a[1], b[nt].z, b[nt].w, d[0], d[1], d[2], d[3]);
+              if (w == 0) mma(d, a[0], b[nt].x, b[nt].y, 0.0f, 0.0f, 0.0f, 0.0f);
+              else mma(d, a[0], b[nt].x, b[nt].y, d[0], d[1], d[2], d[3]);
+              mma(d, a[1], b[nt].z, b[nt].w, d[0], d[1], d[2], d[3]);
             }
           }
         }
+        // the weights' 2^-10, the vectors' power of two: of its exponent, 14 is in the operands
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-          const float f = U == 1 ? to_float(own[j]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j]), (lane & ~3) | u);
+          const float f = 0.0625f * (U == 1 ? to_float(own[j]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j]), (lane & ~3) | u));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            total[j / 2][nt][j % 2 * 2] += f * sum[j / 2][nt][j % 2 * 2];
-            total[j / 2][nt][j % 2 * 2 + 1] += f * sum[j / 2][nt][j % 2 * 2 + 1];
+            total[j / 2][nt][j % 2 * 2] += f * (of_group[nt].x * sum[j / 2][nt][j % 2 * 2]);
+            total[j / 2][nt][j % 2 * 2 + 1] += f * (of_group[nt].y * sum[j / 2][nt][j % 2 * 2 + 1]);
           }
         }
       }
@@ -393,20 +398,26 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
 
 // Of a block with so many warps, for so many operand vectors.
 inline size_t scores_shared(int warps, int64_t groups, int group, int columns, int nt) {
-  return (size_t)warps * kStages * kStageBytes + (size_t)groups * (group / 32) * columns * 64 + 16 + (size_t)warps * kTileRows * 8 * nt * 4;
+  return (size_t)warps * kStages * kStageBytes + (size_t)groups * (group / 32) * columns * 64 + (size_t)groups * 32 * nt + (size_t)warps * kTileRows * 8 * nt * 4;
 }
 constexpr size_t kMostShared = 227 * 1024;
 
 template <typename X, typename S, int GROUP, int NT>
 int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int vectors, void* out, int out_type, int64_t out_stride, cudaStream_t s) {
   auto* kernel = packed_scores_kernel<X, S, GROUP, NT>;
-  const int columns = vectors * OperandOf<X>::parts;
+  const int columns = vectors * PartsOf<X>::value;
   const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows, blocks = ((int64_t)p.groups * GROUP + kBlockColumns - 1) / kBlockColumns;
   int warps = kMostWarps;
   while (scores_shared(warps, p.groups, GROUP, columns, NT) > kMostShared) warps /= 2;
-  // warps share a tile until each has had four tiles' worth of its own, as long as there are columns for each
+  // warps share a tile where that makes the longest warp's work shorter: its rounds over the tiles, each its blocks of columns and
+  // (measured: about half a block's time) what the sums' end takes
   int split = 1;
-  while (split < warps && split < 8 && tiles * split < 148ll * warps * 4 && blocks >= split * 2) split *= 2;
+  double best = 0.0;
+  for (int n = 1; n <= warps && n <= 8 && n <= blocks; n *= 2) {
+    const int64_t teams = 148ll * (warps / n), rounds = (tiles + teams - 1) / teams;
+    const double cost = (double)rounds * ((double)((blocks + n - 1) / n) + 0.6);
+    if (n == 1 || cost < best) split = n, best = cost;
+  }
   // small blocks where there is little for all SMs
   while (warps > split && warps > 2 && tiles * split <= 148ll * warps / 2) warps /= 2;
   const size_t shared = scores_shared(warps, p.groups, GROUP, columns, NT);
@@ -418,7 +429,7 @@ int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int ve
 
 template <typename X, typename S, int GROUP>
 int launch_scores(const mono_packed_t& packed, const mono_matrix_t& x, const mono_matrix_t& out, cudaStream_t s) {
-  constexpr int PARTS = OperandOf<X>::parts;
+  constexpr int PARTS = PartsOf<X>::value;
   const PackedView p = view(packed);
   // vectors of a launch: up to 16 operands, and no more than shared memory has room for beside the stages of two warps
   int most = 16 / PARTS;
