@@ -529,7 +529,8 @@ int mono_timing_read(mono_table* t, mono_timing_t* host_out, int reset);
  *  - No table: the stream is an argument, the work runs on the current device, which has to be the one the
  *    matrices are on, and nothing is allocated or kept, so calls can run at once on several streams (with a workspace each)
  *    and be captured into CUDA graphs.  Descriptors are HOST structs, read before the call returns.
- *  - A matrix that is written must not overlap anything else the call is given.
+ *  - A matrix that is written must not overlap anything else the call is given.  Of a matrix that is read, what lies between
+ *    its rows may be read too (and is not used).
  *  - Products and sums are taken in fp32, and what is written is rounded once, to nearest even.
  *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS, strides up to MONO_MAX_STRIDE (a row of
  *    scores has one column per packed row).
@@ -609,7 +610,7 @@ int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int3
  * Scores of every packed row against a few vectors (a user's vector against all candidates; the output layer that shares
  * the input layer's matrix):  out[m, v] = sum over c of x[m, c] * value(v, c), taken as
  *     sum over groups of  scale(v, group) * (sum over the group's c of x[m, c] * (q(v, c) - 8)),
- * each in fp32, no product rounded to fewer bits.
+ * all sums in fp32 and, but for elements of x below 2^-36 of the largest of their group, no product rounded.
  *  x        [up to MONO_MAX_SCORED, packed->cols]; MONO_ERR_LIMIT for more rows: that is a matrix product
  *  out      [x->rows, packed->rows], any of the types
  * MONO_ERR_LIMIT too for more than MONO_MAX_SCORED_COLS columns.

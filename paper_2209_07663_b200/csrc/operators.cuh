@@ -62,6 +62,59 @@ __device__ __forceinline__ void to_floats(const Vec<T, N>& x, float (&f)[N]) {
   }
 }
 
+// rounded once each, two at a time where two fit a register
+template <typename T, int N>
+__device__ __forceinline__ Vec<T, N> from_floats(const float (&f)[N]) {
+  Vec<T, N> x;
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(f[k], f[k + 1]);
+        memcpy(&x.v[k], &p, 4);
+      } else {
+        const __half2 p = __floats2half2_rn(f[k], f[k + 1]);
+        memcpy(&x.v[k], &p, 4);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x.v[k] = from_float<T>(f[k]);
+  }
+  return x;
+}
+
+// 8 elements from any address: the aligned 16-byte words that hold them, moved by as many bytes as the first one begins behind
+// a multiple of 16.  All of the words have to be readable.
+template <typename T>
+__device__ __forceinline__ void load_shifted(const T* from, uint32_t (&w)[2 * sizeof(T) + 4]) {
+  const uint4* const at = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
+  constexpr int N = sizeof(T) / 2 + 1;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint4 x = __ldg(at + k);
+    w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
+  }
+}
+template <typename T>
+__device__ __forceinline__ Vec<T, 8> shifted(const uint32_t (&in)[2 * sizeof(T) + 4], uint32_t bytes) {
+  constexpr int N = 2 * sizeof(T);                         // words of the 8 elements
+  uint32_t w[N + 4];
+#pragma unroll
+  for (int k = 0; k < N + 4; ++k) w[k] = in[k];
+#pragma unroll
+  for (int k = 0; k < N + 2; ++k) w[k] = bytes & 8 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < N + 1; ++k) w[k] = bytes & 4 ? w[k + 1] : w[k];
+  if (sizeof(T) == 2) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (bytes & 2) * 8);
+  }
+  Vec<T, 8> x;
+  memcpy(&x, w, sizeof(x));
+  return x;
+}
+
 // sum += x, two columns an instruction
 template <int N>
 __device__ __forceinline__ void add_floats(float (&sum)[N], const float (&x)[N]) {

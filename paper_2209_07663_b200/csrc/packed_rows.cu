@@ -82,14 +82,14 @@ __global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* __restrict
 constexpr int kMoves = 4;
 
 template <typename S, typename O, bool ALIGNED, int ROWS>
-__global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView p, int group_words, TokenList tokens, float scale, O* __restrict__ out, int64_t out_stride, int lanes) {
+__global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView p, int group_shift, TokenList tokens, float scale, O* __restrict__ out, int64_t out_stride, int lanes) {
   after_previous_kernel();
   constexpr int PIECES = kMoves / ROWS;
   const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
   const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
   const int words = (p.cols + 7) / 8, w0 = blockIdx.y * lanes * PIECES + lane;
-  uint32_t t[ROWS], q[kMoves];
-  float s[kMoves];
+  uint32_t t[ROWS], q[kMoves] = {};
+  float s[kMoves] = {};
   tokens.rows(row0, groups, t);
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
@@ -97,24 +97,34 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
     const int w = w0 + (k % PIECES) * lanes;
     if (row != kNoToken && w < words) {
       q[k] = __ldg(reinterpret_cast<const uint32_t*>(p.q + row * p.q_stride) + w);
-      s[k] = to_float(static_cast<const S*>(p.scales)[row * p.scale_stride + w / group_words]);
+      s[k] = to_float(static_cast<const S*>(p.scales)[row * p.scale_stride + (w >> group_shift)]);
     }
   }
+  const auto value = [&](bool there, uint32_t nibble, float by) {      // (2^23 + q, less 2^23 + 8)
+    return there ? scale * ((__uint_as_float(0x4B000000u | nibble) - 8388616.0f) * by) : 0.0f;
+  };
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
     const int64_t i = row0 + (k / PIECES) * groups;
     const int w = w0 + (k % PIECES) * lanes;
-    if (i >= tokens.n || w >= words) continue;
-    Vec<O, 8> o;
+    const bool there = t[k / PIECES] != kNoToken;
+    if constexpr (ALIGNED) {
+      if (i >= tokens.n || w >= words) continue;
+      float f[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) o.v[c] = from_float<O>(t[k / PIECES] != kNoToken ? scale * ((float)((int)(q[k] >> (4 * c) & 15) - 8) * s[k]) : 0.0f);
-    O* at = out + i * out_stride + (int64_t)w * 8;
-    if (ALIGNED) {
-      *reinterpret_cast<Vec<O, 8>*>(at) = o;
+      for (int c = 0; c < 8; ++c) f[c] = value(there, q[k] >> (4 * c) & 15, s[k]);
+      *reinterpret_cast<Vec<O, 8>*>(out + i * out_stride + (int64_t)w * 8) = from_floats<O>(f);
     } else {
+      // one column a thread and store, so that neighbours write neighbours: the words are passed round
+      const int near = min(lanes, 32), in = threadIdx.x & (near - 1);
+      O* const to = out + i * out_stride + (int64_t)(w - in) * 8;
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (w * 8 + c < p.cols) at[c] = o.v[c];
+      for (int c = 0; c < 8; ++c) {
+        const int at = c * near + in;                        // among the columns of the threads near by
+        const uint32_t word = __shfl_sync(0xFFFFFFFFu, q[k], at / 8, near);
+        const float by = __shfl_sync(0xFFFFFFFFu, s[k], at / 8, near);
+        if (i < tokens.n && (w - in) * 8 + at < p.cols) to[at] = from_float<O>(value(there, word >> (4 * (at % 8)) & 15, by));
+      }
     }
   }
 }
@@ -126,7 +136,7 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // cores' 16-bit products take 16 rows and 8 vectors at once.  As the bits of an fp16, 4 bits in the lowest places are q * 2^-24 and in
 // the next ones 16 * q * 2^-24, subnormal and exact; times 2^14 or 2^10, less 8 * 2^-10, they are (q - 8) * 2^-10: an AND and
 // a multiply-add for two weights, and a shift for each eight.  (Left subnormal, with the 8 taken off the sums, they took 71 us instead of
-// 74 for 8 vectors against 131072 rows of 4096 columns, and the sums lost three bits.)
+// 75 for 8 vectors against 131072 rows of 4096 columns, and the sums lost three bits.)
 // Vectors become fp16 operands that lose nothing that fp32 sums would keep: those of a group are multiplied by the power of two that takes
 // the largest of them to 2^14 .. 2^15, so that only what is below 2^-36 of it is rounded at all, and fp32 vectors are three operands
 // whose sum they are.  All products are exact, all sums in fp32.
@@ -491,7 +501,7 @@ int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int3
       using S = decltype(s);
       using O = decltype(o);
       const auto launch = [&](auto* kernel) {
-        return launch_operator(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), p, packed->group / 8, list, scale, static_cast<O*>(out->data), out->stride, lanes);
+        return launch_operator(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), p, packed->group == 32 ? 2 : packed->group == 64 ? 3 : 4, list, scale, static_cast<O*>(out->data), out->stride, lanes);
       };
       if (vector_of(*out) == 8) return wide ? launch(packed_token_rows_kernel<S, O, true, 1>) : launch(packed_token_rows_kernel<S, O, true, 4>);
       return wide ? launch(packed_token_rows_kernel<S, O, false, 1>) : launch(packed_token_rows_kernel<S, O, false, 4>);

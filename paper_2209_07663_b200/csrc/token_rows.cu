@@ -12,58 +12,130 @@ constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------
 // Rows by token.  out[i] = scale * weight[token i]: nothing is reused, so bytes bound it.
-// A thread moves VEC columns at once and keeps four such moves in flight behind the read of its token(s): four pieces of one row
-// where rows are wide, one piece of each of four rows where `lanes` threads cover a row.
+// A thread moves VEC columns at once and keeps several such moves in flight behind the read of its token(s): pieces of one row
+// where rows are wide, of four rows where `lanes` threads cover a row.
 // ---------------------------------------------------------------------------
-constexpr int kMoves = 4;
+constexpr int kMoves = 4;                                  // of 4 or 8 columns
 
-template <typename W, typename O, int VEC, int ROWS>
+template <typename W, typename O, int VEC, int ROWS, int MOVES>
 __global__ void __launch_bounds__(kThreads) token_rows_kernel(const W* __restrict__ weight, int64_t weight_stride, TokenList tokens, float scale,
                                                               O* __restrict__ out, int64_t out_stride, int vectors, int lanes) {
   after_previous_kernel();
-  constexpr int PIECES = kMoves / ROWS;
+  constexpr int PIECES = MOVES / ROWS;
   const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
   const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
   const int v0 = blockIdx.y * lanes * PIECES + lane;
   uint32_t t[ROWS];
   tokens.rows(row0, groups, t);
-  Vec<W, VEC> in[kMoves];
+  Vec<W, VEC> in[MOVES];
 #pragma unroll
-  for (int k = 0; k < kMoves; ++k) {
+  for (int k = 0; k < MOVES; ++k) {
     const int r = k / PIECES, v = v0 + (k % PIECES) * lanes;
     if (t[r] != kNoToken && v < vectors) {
       in[k] = *reinterpret_cast<const Vec<W, VEC>*>(weight + t[r] * weight_stride + (int64_t)v * VEC);
     }
   }
 #pragma unroll
-  for (int k = 0; k < kMoves; ++k) {
+  for (int k = 0; k < MOVES; ++k) {
     const int r = k / PIECES, v = v0 + (k % PIECES) * lanes;
     const int64_t i = row0 + r * groups;
     if (i >= tokens.n || v >= vectors) continue;
-    Vec<O, VEC> o;
+    float f[VEC];
+    to_floats(in[k], f);
 #pragma unroll
-    for (int c = 0; c < VEC; ++c) o.v[c] = from_float<O>(t[r] != kNoToken ? scale * to_float(in[k].v[c]) : 0.0f);
-    *reinterpret_cast<Vec<O, VEC>*>(out + i * out_stride + (int64_t)v * VEC) = o;
+    for (int c = 0; c < VEC; ++c) f[c] = t[r] != kNoToken ? scale * f[c] : 0.0f;
+    *reinterpret_cast<Vec<O, VEC>*>(out + i * out_stride + (int64_t)v * VEC) = from_floats<O>(f);
+  }
+}
+
+// The same for rows that begin anywhere: a thread makes pieces of 8 columns that lie on multiples of 16 bytes of `out` (of those that a row begins or ends
+// in, the part that is the row's), from the aligned words that hold them, moved into place in registers.  For rows of 16-bit elements that begin at odd
+// ones: with moves of one column 65536 rows of 1023 bf16 columns took 132 us, with these 67 us (1024 columns: 27).  (With moves of two columns or
+// of one fp32 column they are no faster: 130 bf16 columns 9.5 us against 16.6, 1023 fp32 ones 84 against 89.)
+template <typename W, typename O, int ROWS>
+__global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* __restrict__ weight, int64_t weight_stride, TokenList tokens, float scale,
+                                                                      O* __restrict__ out, int64_t out_stride, int cols, int lanes) {
+  after_previous_kernel();
+  constexpr int PIECES = kMoves / ROWS;
+  const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
+  const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
+  const int v0 = blockIdx.y * lanes * PIECES + lane;
+  const W* const begin = weight;
+  const W* const end = weight + (tokens.vocab - 1) * weight_stride + cols;
+  uint32_t t[ROWS];
+  tokens.rows(row0, groups, t);
+  uint32_t in[kMoves][2 * sizeof(W) + 4];
+#pragma unroll
+  for (int k = 0; k < kMoves; ++k) {
+    const uint32_t row = t[k / PIECES];
+    const int64_t i = row0 + (k / PIECES) * groups;
+    const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(out + i * out_stride) / sizeof(O)) & 7;
+    const int c = (v0 + (k % PIECES) * lanes) * 8 - (int)skew;
+    if (row == kNoToken || c >= cols) continue;
+    const W* const from = weight + row * weight_stride + c;
+    // (the aligned words reach up to 15 bytes beyond the 8 elements, and those up to 7 elements beyond the row)
+    if (from - 16 / sizeof(W) >= begin && from + 8 + 16 / sizeof(W) <= end) {
+      load_shifted(from, in[k]);
+    } else {
+      W x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = c + e >= 0 && c + e < cols ? from[e] : from_float<W>(0.0f);
+      memcpy(in[k], x, sizeof(x));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kMoves; ++k) {
+    const uint32_t row = t[k / PIECES];
+    const int64_t i = row0 + (k / PIECES) * groups;
+    if (i >= tokens.n) continue;
+    const uint32_t skew = (uint32_t)(reinterpret_cast<uintptr_t>(out + i * out_stride) / sizeof(O)) & 7;
+    const int c = (v0 + (k % PIECES) * lanes) * 8 - (int)skew;
+    if (c >= cols) continue;
+    float f[8] = {};
+    if (row != kNoToken) {
+      const W* const from = weight + row * weight_stride + c;
+      const bool whole = from - 16 / sizeof(W) >= begin && from + 8 + 16 / sizeof(W) <= end;
+      to_floats(shifted<W>(in[k], whole ? (uint32_t)reinterpret_cast<uintptr_t>(from) & 15 : 0), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= scale;
+    }
+    const Vec<O, 8> o = from_floats<O>(f);
+    O* const to = out + i * out_stride + c;
+    if (c >= 0 && c + 8 <= cols) {
+      *reinterpret_cast<Vec<O, 8>*>(to) = o;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e >= 0 && c + e < cols) to[e] = o.v[e];
+    }
   }
 }
 
 template <typename W, typename O, int VEC>
 int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, float scale, const mono_matrix_t& out, cudaStream_t s) {
-  const int vectors = (int)(weight.cols / VEC);
-  const auto launch = [&](auto rows_of_a_thread, int lanes) {
-    constexpr int ROWS = decltype(rows_of_a_thread)::value;
-    const int64_t rows = (int64_t)(kThreads / lanes) * ROWS, columns = (int64_t)lanes * (kMoves / ROWS);
-    const dim3 grid((unsigned)((tokens.n + rows - 1) / rows), (unsigned)((vectors + columns - 1) / columns));
-    return launch_operator(token_rows_kernel<W, O, VEC, ROWS>, grid, kThreads, 0, s, static_cast<const W*>(weight.data), weight.stride, tokens, scale,
-                           static_cast<O*>(out.data), out.stride, vectors, lanes);
+  constexpr int MOVES = VEC >= 4 ? kMoves : kMoves * 4 / VEC;      // (narrow moves: as many bytes in flight)
+  const bool shifts = VEC == 1 && sizeof(W) == 2 && weight.cols >= 32;      // (a few columns are a piece or two whichever way)
+  const int vectors = shifts ? (int)((weight.cols + 7 + 7) / 8) : (int)(weight.cols / VEC), moves = shifts ? kMoves : MOVES;
+  const auto lanes_for = [&](int pieces) {
+    int lanes = 1;
+    while (lanes < kThreads && lanes * pieces < vectors) lanes *= 2;
+    return lanes;
   };
-  int lanes = 1;
-  if (vectors > 64) {
-    while (lanes < kThreads && lanes * kMoves < vectors) lanes *= 2;
-    return launch(Width<1>(), lanes);
-  }
-  while (lanes < vectors) lanes *= 2;
-  return launch(Width<4>(), lanes);
+  const auto launch = [&](auto rows_of_a_thread) {
+    constexpr int ROWS = decltype(rows_of_a_thread)::value;
+    const int pieces = moves / ROWS, lanes = lanes_for(pieces);
+    const int64_t rows = (int64_t)(kThreads / lanes) * ROWS, columns = (int64_t)lanes * pieces;
+    const dim3 grid((unsigned)((tokens.n + rows - 1) / rows), (unsigned)((vectors + columns - 1) / columns));
+    const auto* from = static_cast<const W*>(weight.data);
+    auto* to = static_cast<O*>(out.data);
+    if constexpr (VEC == 1 && sizeof(W) == 2) {
+      if (shifts)
+        return launch_operator(token_rows_shifted_kernel<W, O, ROWS>, grid, kThreads, 0, s, from, weight.stride, tokens, scale, to, out.stride, (int)weight.cols, lanes);
+    }
+    return launch_operator(token_rows_kernel<W, O, VEC, ROWS, MOVES>, grid, kThreads, 0, s, from, weight.stride, tokens, scale, to, out.stride, vectors, lanes);
+  };
+  // one row a thread where rows are wide, or leave fewer moves idle that way (130 bf16 columns in moves of two: 9.5 us against 13.2)
+  return vectors > 256 || lanes_for(moves) * moves < lanes_for(moves / 4) * (moves / 4) ? launch(Width<1>()) : launch(Width<4>());
 }
 
 // ---------------------------------------------------------------------------
@@ -426,13 +498,10 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 && !ADD ? 3 : 2) sum_rows_k
               O* at = to + (int64_t)e[u].row * out.stride;
 #pragma unroll
               for (int r = 0; r < R; ++r) {
-                Vec<O, VEC> o;
+                float f[VEC];
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) {
-                  if constexpr (ADD) o.v[c] = from_float<O>(to_float(old[u][r].v[c]) + out.scale * sum[r][c]);
-                  else o.v[c] = from_float<O>(out.scale * sum[r][c]);
-                }
-                if (mine[r]) *reinterpret_cast<Vec<O, VEC>*>(at + r * lanes * VEC) = o;
+                for (int c = 0; c < VEC; ++c) f[c] = ADD ? to_float(old[ADD ? u : 0][r].v[c]) + out.scale * sum[r][c] : out.scale * sum[r][c];
+                if (mine[r]) *reinterpret_cast<Vec<O, VEC>*>(at + r * lanes * VEC) = from_floats<O>(f);
               }
             } else {
               float* keep = piece + (group * 2 + (began_before ? 0 : 1)) * width + lane * VEC;
