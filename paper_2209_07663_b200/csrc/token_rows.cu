@@ -116,14 +116,11 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
   constexpr int MOVES = VEC >= 4 ? kMoves : kMoves * 4 / VEC;      // (narrow moves: as many bytes in flight)
   const bool shifts = VEC == 1 && sizeof(W) == 2 && weight.cols >= 32;      // (a few columns are a piece or two whichever way)
   const int vectors = shifts ? (int)((weight.cols + 7 + 7) / 8) : (int)(weight.cols / VEC), moves = shifts ? kMoves : MOVES;
-  const auto lanes_for = [&](int pieces) {
-    int lanes = 1;
-    while (lanes < kThreads && lanes * pieces < vectors) lanes *= 2;
-    return lanes;
-  };
   const auto launch = [&](auto rows_of_a_thread) {
     constexpr int ROWS = decltype(rows_of_a_thread)::value;
-    const int pieces = moves / ROWS, lanes = lanes_for(pieces);
+    const int pieces = moves / ROWS;
+    int lanes = 1;
+    while (lanes < kThreads && lanes * pieces < vectors) lanes *= 2;
     const int64_t rows = (int64_t)(kThreads / lanes) * ROWS, columns = (int64_t)lanes * pieces;
     const dim3 grid((unsigned)((tokens.n + rows - 1) / rows), (unsigned)((vectors + columns - 1) / columns));
     const auto* from = static_cast<const W*>(weight.data);
@@ -134,8 +131,8 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
     }
     return launch_operator(token_rows_kernel<W, O, VEC, ROWS, MOVES>, grid, kThreads, 0, s, from, weight.stride, tokens, scale, to, out.stride, vectors, lanes);
   };
-  // one row a thread where rows are wide, or leave fewer moves idle that way (130 bf16 columns in moves of two: 9.5 us against 13.2)
-  return vectors > 256 || lanes_for(moves) * moves < lanes_for(moves / 4) * (moves / 4) ? launch(Width<1>()) : launch(Width<4>());
+  // (65536 rows of 1024 bf16 columns: one row a thread 27 us, four 32 us)
+  return vectors > 64 ? launch(Width<1>()) : launch(Width<4>());
 }
 
 // ---------------------------------------------------------------------------
