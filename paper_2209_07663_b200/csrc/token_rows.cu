@@ -149,12 +149,12 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
 // Where all of the gradient is written, its zeros are filled in by blocks behind those that sort, which
 // use a few SMs for a few microseconds; the rows that tokens name are written again by the sums.
 // ---------------------------------------------------------------------------
-constexpr int64_t kSmallTokens = 256;
+constexpr int64_t kSmallTokens = 512;
+constexpr int kSmallRun = 2;                                // their positions of a group
 constexpr int64_t kRankTokens = 8192;
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortKeys = 8;                               // keys of a thread
-constexpr int kSortTile = kSortThreads * kSortKeys;
+constexpr int kMostSortKeys = 8;                           // keys of a thread
 constexpr int kMaxDigitBits = 9;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
 static_assert(kMaxDigits == kSortThreads, "a thread has one digit's counts");
@@ -236,9 +236,14 @@ __device__ __forceinline__ uint32_t count_before(const uint32_t* keys, int from,
   return n;
 }
 
+// Lets the launch of the kernel behind this one begin; it waits for this one's end itself (after_previous_kernel).  The kernels of a
+// gradient are short and leave SMs free (with it and few keys a thread in the sort, 16384 tokens of 1024 columns went from 40 to 34 us).
+__device__ __forceinline__ void release_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // 32 tokens a block; each warp counts over its share of all tokens.
 __global__ void __launch_bounds__(kThreads) rank_tokens_kernel(TokenList tokens, Entry* __restrict__ sorted, Zeros zeros) {
   after_previous_kernel();
+  release_next_kernel();
   if (zeros.here()) { zeros.fill(); return; }
   constexpr int kWarps = kThreads / 32;
   __shared__ uint32_t keys[kRankTokens];
@@ -266,9 +271,11 @@ __global__ void __launch_bounds__(kThreads) rank_tokens_kernel(TokenList tokens,
 }
 
 // (marks: cleared, by the blocks that would fill zeros, where this is the first pass)
+template <int KEYS>
 __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, int64_t n, int shift, int bits, uint32_t* __restrict__ counts, uint4* marks, int64_t mark_words,
                                                                     Zeros zeros) {
   after_previous_kernel();
+  release_next_kernel();
   if (zeros.here()) {
     if (!marks) { zeros.fill(); return; }
     for (int64_t i = (int64_t)(blockIdx.x - zeros.first) * kSortThreads + threadIdx.x; i < mark_words; i += (int64_t)(gridDim.x - zeros.first) * kSortThreads)
@@ -278,11 +285,11 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, i
   __shared__ uint32_t count[kMaxDigits];
   count[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
-  Entry e[kSortKeys];
+  const int64_t base = (int64_t)blockIdx.x * (kSortThreads * KEYS);
+  Entry e[KEYS];
   keys.load(base + threadIdx.x, kSortThreads, e);
 #pragma unroll
-  for (int k = 0; k < kSortKeys; ++k)
+  for (int k = 0; k < KEYS; ++k)
     if (e[k].row != kBehind) atomicAdd(&count[(e[k].row >> shift) & ((1 << bits) - 1)], 1u);
   __syncthreads();
   counts[(int64_t)blockIdx.x * kMaxDigits + threadIdx.x] = count[threadIdx.x];
@@ -299,17 +306,19 @@ __global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t
 }
 
 // A key goes behind the keys of lower digits of all tiles, those of its digit in earlier tiles, in earlier warps of its tile (warp w has the
-// tile's keys [w * 256, (w + 1) * 256)), in earlier rounds of 32 keys, and at lower lanes (__match_any_sync).
+// tile's keys [w * 32 * KEYS, (w + 1) * 32 * KEYS)), in earlier rounds of 32 keys, and at lower lanes.
+template <int KEYS>
 __global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, int64_t n, int shift, int bits, const uint32_t* __restrict__ counts, int64_t tiles,
                                                                     const uint32_t* __restrict__ coarse, Entry* __restrict__ sorted, uint8_t* marks, Zeros zeros) {
   after_previous_kernel();
+  release_next_kernel();
   if (zeros.here()) { zeros.fill(); return; }
   __shared__ __align__(8) uint32_t next[kSortWarps][kMaxDigits];        // counts of the warps, then the place of a warp's next key of a digit
   __shared__ uint32_t warp_sum[kSortWarps];
   const int digits = 1 << bits, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t tile = blockIdx.x, base = tile * kSortTile + warp * (32 * kSortKeys);
+  const int64_t tile = blockIdx.x, base = tile * (kSortThreads * KEYS) + warp * (32 * KEYS);
   if (tile == 0 && threadIdx.x == 0) sorted[n] = {kBehind, 0};
-  Entry e[kSortKeys];
+  Entry e[KEYS];
   keys.load(base + lane, 32, e);
   if (marks) {
     // Of the tile's keys that share a cell, the last one to write it marks its row and those of the same row leave it alone: marked by every
@@ -317,14 +326,14 @@ __global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, i
     uint64_t* cell = reinterpret_cast<uint64_t*>(next[0]);
     constexpr uint32_t kCells = sizeof(next) / 8;
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k)
-      if (e[k].row < keys.tokens.vocab) cell[e[k].row % kCells] = (uint64_t)e[k].row << 32 | (threadIdx.x * kSortKeys + k);
+    for (int k = 0; k < KEYS; ++k)
+      if (e[k].row < keys.tokens.vocab) cell[e[k].row % kCells] = (uint64_t)e[k].row << 32 | (threadIdx.x * KEYS + k);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
+    for (int k = 0; k < KEYS; ++k) {
       if (e[k].row >= keys.tokens.vocab) continue;
       const uint64_t by = cell[e[k].row % kCells];
-      if ((uint32_t)(by >> 32) != e[k].row || (uint32_t)by == threadIdx.x * kSortKeys + k) marks[e[k].row] = 1;
+      if ((uint32_t)(by >> 32) != e[k].row || (uint32_t)by == threadIdx.x * KEYS + k) marks[e[k].row] = 1;
     }
     __syncthreads();
   }
@@ -352,7 +361,7 @@ __global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, i
   for (int w = 0; w < kSortWarps; ++w) next[w][threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kSortKeys; ++k)
+  for (int k = 0; k < KEYS; ++k)
     if (e[k].row != kBehind) atomicAdd(&next[warp][(e[k].row >> shift) & (digits - 1)], 1u);
   uint32_t scan = total;
 #pragma unroll
@@ -373,10 +382,14 @@ __global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, i
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kSortKeys; ++k) {
+  for (int k = 0; k < KEYS; ++k) {
     const bool there = e[k].row != kBehind;
-    const uint32_t digit = there ? (e[k].row >> shift) & (digits - 1) : kMaxDigits;
-    const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+    const uint32_t digit = (e[k].row >> shift) & (digits - 1);
+    uint32_t same = __ballot_sync(0xFFFFFFFFu, there);       // lanes whose digits agree in every bit
+    for (int b = 0; b < bits; ++b) {
+      const uint32_t set = __ballot_sync(0xFFFFFFFFu, digit >> b & 1);
+      same &= digit >> b & 1 ? set : ~set;
+    }
     const uint32_t rank = __popc(same & ((1u << lane) - 1));
     uint32_t to = 0;
     if (there) to = next[warp][digit] + rank;
@@ -406,13 +419,14 @@ struct GradOut {
 // ADD: what is there is added to.  It is read with the terms, ahead of the sum that it waits for: a row at a time, a
 // thread's reads would come one after the other.
 // blockIdx.x: runs of `run` positions, one for each group of `lanes` threads; blockIdx.y: part_vectors vectors of VEC columns.
-// Without `sorted` (at most kSmallTokens tokens, all in the runs of one block) the block sorts the tokens itself.
+// Without `sorted` (at most kSmallTokens tokens) every block sorts all tokens itself.
 template <typename G, typename O, int VEC, bool ADD>
-__global__ void __launch_bounds__(kThreads, VEC >= 4 && !ADD ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
+__global__ void __launch_bounds__(kThreads, VEC == 1 || (VEC >= 4 && !ADD) ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
                                                                                        int run, GradOut<O> out, int part_vectors, int lanes) {
   after_previous_kernel();
+  release_next_kernel();
   constexpr int R = kLaneColumns / VEC;
-  constexpr int U = 4;      // positions whose terms are in flight at once
+  constexpr int U = VEC == 1 ? 2 : 4;                       // positions whose terms are in flight at once
   constexpr uint32_t kNone = 0xFFFFFFFFu;
   __shared__ float piece[2 * kThreads * kLaneColumns];      // [groups][2][lanes * kLaneColumns]: front, end
   __shared__ uint2 pieces[2 * kThreads];                    // of the pieces there are, in order: the row, the place in piece[]
@@ -420,19 +434,39 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 && !ADD ? 3 : 2) sum_rows_k
   __shared__ uint32_t keys[kSmallTokens];
   __shared__ Entry ranked[kSmallTokens + 1];
   const int64_t n = tokens.n;
-  if (sorted == nullptr) {
+  const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes, width = lanes * kLaneColumns;
+  int64_t b0 = (int64_t)blockIdx.x * groups * run, b1 = b0 + (int64_t)groups * run < n ? b0 + (int64_t)groups * run : n;
+  const bool here = sorted == nullptr;
+  if (here) {
+    constexpr int K = kSmallTokens / kThreads;
     const Keys all{tokens, nullptr};
-    Entry own[1];
-    all.load(threadIdx.x, 1, own);
-    keys[threadIdx.x] = own[0].row;
+    Entry own[K];
+    all.load(threadIdx.x, kThreads, own);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (own[k].row != kBehind) keys[own[k].at] = own[k].row;
     __syncthreads();
-    if (threadIdx.x < n) ranked[count_before(keys, 0, (int)n, keys[threadIdx.x], threadIdx.x)] = {keys[threadIdx.x], threadIdx.x};
+#pragma unroll 1
+    for (int k = 0; k < K; ++k) {
+      const int i = threadIdx.x + k * kThreads;
+      if (i < n) ranked[count_before(keys, 0, (int)n, keys[i], i)] = {keys[i], (uint32_t)i};
+    }
     if (threadIdx.x == 0) ranked[n] = {kBehind, 0};
     __syncthreads();
     sorted = ranked;
+    // the rows that begin among the block's positions, to their ends: no other block has a part in them
+    const auto behind = [&](int64_t p) {                    // the first position behind the row of position p
+      int64_t low = p, high = n;                            // (of the row; not of it, or n)
+      while (high - low > 1) {
+        const int64_t mid = (low + high) / 2;
+        if (ranked[mid].row == ranked[p].row) low = mid; else high = mid;
+      }
+      return high;
+    };
+    if (b0 > 0 && ranked[b0].row == ranked[b0 - 1].row) b0 = behind(b0);
+    b1 = b0 >= b1 ? b0 : behind(b1 - 1);
+    run = (int)((b1 - b0 + groups - 1) / groups);
   }
-  const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes, width = lanes * kLaneColumns;
-  const int64_t b0 = (int64_t)blockIdx.x * groups * run, b1 = b0 + (int64_t)groups * run < n ? b0 + (int64_t)groups * run : n;
   const int64_t p0 = b0 + (int64_t)group * run;
   const int first = blockIdx.y * part_vectors, end = min(first + part_vectors, out.cols / VEC);
   uint32_t front_row = kNone, end_row = kNone;
@@ -544,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 && !ADD ? 3 : 2) sum_rows_k
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) count += warp_pieces[w];
   if (count == 0) return;
-  const uint32_t before_row = b0 > 0 ? sorted[b0 - 1].row : kNone, behind_row = b1 < n ? sorted[b1].row : kNone;
+  const uint32_t before_row = b0 > 0 && !here ? sorted[b0 - 1].row : kNone, behind_row = b1 < n && !here ? sorted[b1].row : kNone;
   for (int c = threadIdx.x; c < (end - first) * VEC; c += kThreads) {
     constexpr int K = 8;
     const int column = first * VEC + c;
@@ -615,6 +649,7 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* __rest
 
 struct SortPlan {
   int passes, bits;                                        // digits of `bits` bits each
+  int keys;                                                // of a thread
   int64_t tiles, coarse;
 };
 
@@ -624,7 +659,11 @@ SortPlan plan_sort(int64_t n, int64_t vocab) {
   SortPlan p;
   p.passes = (width + kMaxDigitBits - 1) / kMaxDigitBits;
   p.bits = (width + p.passes - 1) / p.passes;
-  p.tiles = (n + kSortTile - 1) / kSortTile;
+  // few keys a thread spread the work; up to kMaxFineTiles tiles are counted without another launch
+  p.keys = 1;
+  while (p.keys < kMostSortKeys && n > (int64_t)kSortThreads * p.keys * kMaxFineTiles) p.keys *= 2;
+  const int64_t tile = (int64_t)kSortThreads * p.keys;
+  p.tiles = (n + tile - 1) / tile;
   p.coarse = p.tiles > kMaxFineTiles ? (p.tiles + kCoarse - 1) / kCoarse : 0;
   return p;
 }
@@ -646,7 +685,7 @@ SumPlan plan_sums(int64_t n, int vectors, int vec) {
   // long runs have fewer pieces, short ones more warps: as long as there are 24 warps for every SM
   p.run = kMaxRun;
   while (p.run > kMinRun && n * p.parts / p.run * p.lanes / 32 < 148 * 24) p.run /= 2;
-  if (n <= kSmallTokens) p.run = std::max(1, (int)((n + p.groups - 1) / p.groups));
+  if (n <= kSmallTokens) p.run = kSmallRun;
   p.blocks = (n + (int64_t)p.run * p.groups - 1) / ((int64_t)p.run * p.groups);
   return p;
 }
@@ -744,12 +783,19 @@ int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale,
       zeros.marks = pass == 0 ? nullptr : marks;
       Zeros z = share(2 * pass - skipped, shares, p.tiles, &grid);
       if (marked) { z.first = (unsigned)p.tiles; grid = dim3((unsigned)p.tiles + 16); }
-      if ((rc = launch_operator(count_digits_kernel, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, reinterpret_cast<uint4*>(marked), (vocab + 15) / 16, z)) != MONO_OK)
-        return rc;
+      const auto with_keys = [&](auto f) { return with_width(p.keys, f); };
+      rc = with_keys([&](auto k) {
+        return launch_operator(count_digits_kernel<decltype(k)::value>, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, reinterpret_cast<uint4*>(marked),
+                               (vocab + 15) / 16, z);
+      });
+      if (rc != MONO_OK) return rc;
       if (p.coarse && (rc = launch_operator(sum_counts_kernel, dim3((unsigned)p.coarse), kSortThreads, 0, s, w.counts, p.tiles, w.coarse)) != MONO_OK) return rc;
       z = share(2 * pass + 1 - skipped, shares, p.tiles, &grid);
-      if ((rc = launch_operator(scatter_keys_kernel, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, p.tiles, p.coarse ? w.coarse : nullptr, place, marked, z)) != MONO_OK)
-        return rc;
+      rc = with_keys([&](auto k) {
+        return launch_operator(scatter_keys_kernel<decltype(k)::value>, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, p.tiles, p.coarse ? w.coarse : nullptr, place,
+                               marked, z);
+      });
+      if (rc != MONO_OK) return rc;
       sorted = place;
       place = place == w.a ? w.b : w.a;
     }
@@ -758,7 +804,7 @@ int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale,
     return launch_operator(kernel, sum_grid, kThreads, 0, s, from, (uint32_t)(grad.stride * (int64_t)sizeof(G)), tokens, sorted, sums.run, to, sums.part_vectors, sums.lanes);
   };
   rc = accumulate ? sum(sum_rows_kernel<G, O, VEC, true>) : sum(sum_rows_kernel<G, O, VEC, false>);
-  if (rc != MONO_OK || sums.blocks < 2) return rc;
+  if (rc != MONO_OK || sums.blocks < 2 || n <= kSmallTokens) return rc;
   constexpr int JOINED = std::min(4, VEC);
   const int joined = cols / JOINED, threads = joined >= kThreads ? kThreads : (joined + 31) / 32 * 32;
   return launch_operator(join_rows_kernel<O, JOINED>, dim3((unsigned)(sums.blocks - 1), (unsigned)((joined + threads - 1) / threads)), threads, 0, s, sorted, n, sums.run * sums.groups,

@@ -144,7 +144,7 @@ def test_rows_behind_the_32nd_bit():
 
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("dim", [1, 2, 7, 8, 36, 64, 100, 257, 515, 1024])
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 129, 255, 256, 257, 1000, 2049, 5000, 8192, 8193])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 129, 255, 256, 257, 500, 512, 513, 1000, 2049, 5000, 8192, 8193])
 def test_gradient_of_many_sizes(n, dim, accumulate):
     vocab = (3, 300, 1000)[n % 3]
     for k, (g, o) in enumerate(itertools.product(TYPES, TYPES)):
@@ -166,7 +166,7 @@ def test_gradient_of_many_vocabularies(vocab):
         check_grad(got, None, grad, tokens, 1.0, -1, f"{n}")
 
 
-@pytest.mark.parametrize("n", [64, 128, 4096, 4160, 70000])
+@pytest.mark.parametrize("n", [64, 128, 300, 512, 4096, 4160, 70000])
 def test_gradient_of_one_row_and_of_rows_that_end_with_a_chunk(n):
     grad = randn(n, 72, dtype=BF16)
     for tokens in (torch.full((n,), 4, device="cuda"), torch.arange(n, device="cuda") // 64, torch.arange(n, device="cuda") // 32 % 9,
