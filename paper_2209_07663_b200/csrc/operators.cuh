@@ -221,7 +221,9 @@ inline int launch_operator(const Launch& l, void (*kernel)(P...), A&&... args) {
   attr[1].val.clusterDim = {l.cluster, 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = l.cluster ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess ? MONO_OK : MONO_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess) return MONO_OK;
+  cudaGetLastError();                                       // (reported here, not by the next call that asks)
+  return MONO_ERR_CUDA;
 }
 template <typename... P, typename... A>
 inline int launch_operator(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, cudaStream_t s, A&&... args) {

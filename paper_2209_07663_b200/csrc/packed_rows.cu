@@ -151,9 +151,10 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // 32 rows, a run of columns each.  Scales are read ahead by the four threads of a row, one each.
 // ---------------------------------------------------------------------------
 constexpr int kTileRows = 32;
-constexpr int kBlockColumns = 128, kBlockBytes = kBlockColumns / 2;
-constexpr int kMostWarps = 16;
-constexpr int kStages = 4;
+constexpr int kBlockColumns = 256, kBlockBytes = kBlockColumns / 2;
+constexpr int kRowMoves = kBlockBytes / 16, kMoveRows = 32 / kRowMoves;      // 16-byte moves of a row, rows of a warp's moves
+constexpr int kMostWarps = 12;
+constexpr int kStages = 3;
 constexpr int kStageBytes = kTileRows * kBlockBytes;
 
 template <typename X> struct PartsOf { static constexpr int value = 1; };
@@ -185,7 +186,7 @@ __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y)
 
 template <int BYTES> struct alignas(BYTES) Words { uint32_t w[BYTES / 4]; };
 
-// Shared memory: the warps' stages, [warps][kStages][32][64 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; of each group, [4 * NT]
+// Shared memory: the warps' stages, [warps][kStages][32][128 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; of each group, [4 * NT]
 // pairs of columns: the powers of two; the sums of the warps, [warps][32][8 * NT].  `columns` operands:
 // vectors, or the parts of vectors.
 template <typename X, typename S, int GROUP, int NT>
@@ -210,31 +211,35 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
   const int row_bytes = (p.cols + 31) / 32 * 16;
   const int64_t step = (int64_t)gridDim.x * teams, tile0 = (int64_t)blockIdx.x * teams + team;
 
-  // A stage: the lane has 16 bytes of rows lane / 4, lane / 4 + 8, ...  Where they go is turned by the row, so that the threads that read
-  // a group together find their bytes in different banks.
+  // A stage: the lane has 16 bytes of every kMoveRows-th row.  Where they go is turned by the row, so that the threads that read a group
+  // together (of two, four or eight rows at a time) find their bytes in different banks.
   uint4* const stages = shared + warp * kStages * (kStageBytes / 16);
-  const auto turned = [](int row, int piece) { return row * 4 + (piece ^ (GROUP == 128 ? 0 : GROUP == 64 ? row & 2 : row >> 1 & 3)); };
+  const auto turned = [](int row, int piece) {
+    const int turn = row / (8 / kRowMoves);                 // (rows that lie in the same banks)
+    return row * kRowMoves + (piece ^ ((GROUP == 128 ? turn << 2 : GROUP == 64 ? turn << 1 : turn) & (kRowMoves - 1)));
+  };
+  const int move_row = lane / kRowMoves, move_at = lane % kRowMoves * 16;
   int64_t fill_tile = tile0;
   int fill_k = k0, fill_stage = 0;
-  const uint8_t* fill_from[kTileRows / 8];                  // the lane's bytes of its rows
-  const uint32_t fill_to = (uint32_t)__cvta_generic_to_shared(stages) + turned(g, t) * 16;
+  const uint8_t* fill_from[kTileRows / kMoveRows];          // the lane's bytes of its rows
   const auto fill = [&] {
     if (fill_tile < tiles) {
       if (fill_k == k0) {
 #pragma unroll
-        for (int i = 0; i < kTileRows / 8; ++i) fill_from[i] = p.q + min(fill_tile * kTileRows + g + 8 * i, p.rows - 1) * p.q_stride + (k0 * kBlockBytes + t * 16);
+        for (int i = 0; i < kTileRows / kMoveRows; ++i)
+          fill_from[i] = p.q + min(fill_tile * kTileRows + move_row + kMoveRows * i, p.rows - 1) * p.q_stride + (k0 * kBlockBytes + move_at);
       }
-      if (fill_k * kBlockBytes + t * 16 < row_bytes) {      // (behind the row's end the vectors are zero, whatever the stage holds)
-        const uint32_t to = fill_to + fill_stage * kStageBytes;
+      if (fill_k * kBlockBytes + move_at < row_bytes) {     // (behind the row's end the vectors are zero, whatever the stage holds)
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(stages) + fill_stage * kStageBytes;
 #pragma unroll
-        for (int i = 0; i < kTileRows / 8; ++i) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 8 * kBlockBytes), "l"(fill_from[i]) : "memory");
+        for (int i = 0; i < kTileRows / kMoveRows; ++i) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + turned(move_row + kMoveRows * i, lane % kRowMoves) * 16), "l"(fill_from[i]) : "memory");
           fill_from[i] += kBlockBytes;
         }
       }
       if (++fill_k >= k1) { fill_k = k0; fill_tile += step; }
     }
-    fill_stage = (fill_stage + 1) % kStages;
+    fill_stage = fill_stage + 1 == kStages ? 0 : fill_stage + 1;
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll 1
@@ -288,16 +293,20 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
     }
   }
 
-  S scales[SETS];                                           // of group t (modulo U) of the next block of columns
+  constexpr int SCALES = (U + 3) / 4;
+  S scales[SETS][SCALES];                                   // of groups t, t + 4 (modulo U) of the next block of columns
   const S* scale_row[SETS];
   const auto load_scales = [&](int64_t tile, int k) {
     if (k == k0) {
 #pragma unroll
       for (int j = 0; j < SETS; ++j) scale_row[j] = static_cast<const S*>(p.scales) + min(tile * kTileRows + g + 8 * j, p.rows - 1) * p.scale_stride;
     }
-    const int at = min(k * U + (t & (U - 1)), p.groups - 1);
 #pragma unroll
-    for (int j = 0; j < SETS; ++j) scales[j] = scale_row[j][at];
+    for (int u = 0; u < SCALES; ++u) {
+      const int at = min(k * U + u * 4 + (t & (U - 1)), p.groups - 1);
+#pragma unroll
+      for (int j = 0; j < SETS; ++j) scales[j][u] = scale_row[j][at];
+    }
   };
   if (tile0 < tiles) load_scales(tile0, k0);
   int operand[NT];                                          // in shared[]; for a column that there is none of another one's: its sums are not written
@@ -318,13 +327,16 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
       __syncwarp();                                         // the stage is there for the warp, and it is done with the one that is filled now
       fill();
-      S own[SETS];
+      S own[SETS][SCALES];
 #pragma unroll
-      for (int j = 0; j < SETS; ++j) own[j] = scales[j];
+      for (int j = 0; j < SETS; ++j) {
+#pragma unroll
+        for (int u = 0; u < SCALES; ++u) own[j][u] = scales[j][u];
+      }
       const bool same = k + 1 < k1;
       if (same || tile + step < tiles) load_scales(same ? tile : tile + step, same ? k + 1 : k0);
       const int from = stage_bytes + stage * kStageBytes;
-      stage = (stage + 1) % kStages;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (k * U + u >= p.groups) break;
@@ -367,7 +379,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
         // the weights' 2^-10, the vectors' power of two: of its exponent, 14 is in the operands
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-          const float f = 0.0625f * (U == 1 ? to_float(own[j]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j]), (lane & ~3) | u));
+          const float f = 0.0625f * (U == 1 ? to_float(own[j][0]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4)));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             total[j / 2][nt][j % 2 * 2] += f * (of_group[nt].x * sum[j / 2][nt][j % 2 * 2]);
@@ -418,18 +430,19 @@ int launch_scores_tile(const PackedView& p, const X* x, int64_t x_stride, int ve
   const int columns = vectors * PartsOf<X>::value;
   const int64_t tiles = (p.rows + kTileRows - 1) / kTileRows, blocks = ((int64_t)p.groups * GROUP + kBlockColumns - 1) / kBlockColumns;
   int warps = kMostWarps;
+  while (warps > 8 && scores_shared(warps, p.groups, GROUP, columns, NT) > kMostShared) warps -= 4;
   while (scores_shared(warps, p.groups, GROUP, columns, NT) > kMostShared) warps /= 2;
   // warps share a tile where that makes the longest warp's work shorter: its rounds over the tiles, each its blocks of columns and
   // (measured: about half a block's time) what the sums' end takes
   int split = 1;
   double best = 0.0;
-  for (int n = 1; n <= warps && n <= 8 && n <= blocks; n *= 2) {
+  for (int n = 1; warps % n == 0 && n <= 8 && n <= blocks; n *= 2) {
     const int64_t teams = 148ll * (warps / n), rounds = (tiles + teams - 1) / teams;
     const double cost = (double)rounds * ((double)((blocks + n - 1) / n) + 0.6);
     if (n == 1 || cost < best) split = n, best = cost;
   }
   // small blocks where there is little for all SMs
-  while (warps > split && warps > 2 && tiles * split <= 148ll * warps / 2) warps /= 2;
+  while (warps / 2 % split == 0 && warps > 3 && tiles * split <= 148ll * warps / 2) warps /= 2;
   const size_t shared = scores_shared(warps, p.groups, GROUP, columns, NT);
   const int teams = warps / split;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared) != cudaSuccess) return MONO_ERR_CUDA;

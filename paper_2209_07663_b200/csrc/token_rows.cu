@@ -421,18 +421,22 @@ struct GradOut {
 // blockIdx.x: runs of `run` positions, one for each group of `lanes` threads; blockIdx.y: part_vectors vectors of VEC columns.
 // Without `sorted` (at most kSmallTokens tokens) every block sorts all tokens itself.
 template <typename G, typename O, int VEC, bool ADD>
-__global__ void __launch_bounds__(kThreads, VEC == 1 || (VEC >= 4 && !ADD) ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
+__global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) == 2) ? (ADD ? 2 : 3) : VEC == 1 ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
                                                                                        int run, GradOut<O> out, int part_vectors, int lanes) {
   after_previous_kernel();
   release_next_kernel();
   constexpr int R = kLaneColumns / VEC;
-  constexpr int U = VEC == 1 ? 2 : 4;                       // positions whose terms are in flight at once
+  // Rows of 16-bit elements that begin anywhere: a thread has 8 neighbouring columns of the terms, from the aligned words that hold them, and what
+  // it writes passes through shared memory, so that neighbours write neighbours.
+  constexpr bool SHIFTED = VEC == 1 && sizeof(G) == 2;
+  constexpr int U = VEC == 1 && !SHIFTED ? 2 : 4;           // positions whose terms are in flight at once
   constexpr uint32_t kNone = 0xFFFFFFFFu;
   __shared__ float piece[2 * kThreads * kLaneColumns];      // [groups][2][lanes * kLaneColumns]: front, end
   __shared__ uint2 pieces[2 * kThreads];                    // of the pieces there are, in order: the row, the place in piece[]
   __shared__ uint32_t warp_pieces[kThreads / 32];
   __shared__ uint32_t keys[kSmallTokens];
   __shared__ Entry ranked[kSmallTokens + 1];
+  __shared__ __align__(16) float turned[SHIFTED ? kThreads * kLaneColumns : 1];
   const int64_t n = tokens.n;
   const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes, width = lanes * kLaneColumns;
   int64_t b0 = (int64_t)blockIdx.x * groups * run, b1 = b0 + (int64_t)groups * run < n ? b0 + (int64_t)groups * run : n;
@@ -484,19 +488,40 @@ __global__ void __launch_bounds__(kThreads, VEC == 1 || (VEC >= 4 && !ADD) ? 3 :
     for (int r = 0; r < R; ++r) mine[r] = first + lane + r * lanes < end;
     const char* const from = reinterpret_cast<const char*>(grad) + (int64_t)(first + lane) * (VEC * sizeof(G));
     O* const to = out.data + (int64_t)(first + lane) * VEC;
+    const G* const grad_end = grad + (n - 1) * (int64_t)(grad_stride / sizeof(G)) + out.cols;
+    const uint32_t near = lanes == 32 ? 0xFFFFFFFFu : ((1u << lanes) - 1) << (threadIdx.x % 32 & ~(lanes - 1));      // the group's threads
     Entry e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) e[u] = list[min(u, len)];
     bool began_before = p0 > 0 && list[-1].row == e[0].row;
 
     for (int i = 0; i < len; i += U) {
-      Vec<G, VEC> term[U][R];
+      Vec<G, VEC> term[SHIFTED ? 1 : U][R];
+      uint32_t raw[SHIFTED ? U : 1][8], begins[SHIFTED ? U : 1];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const char* row = from + (uint64_t)e[u].at * grad_stride;
+        if constexpr (SHIFTED) {
+          const G* const at = reinterpret_cast<const G*>(row) + lane * 7;       // (from is the lane's first column of one)
+          const bool whole = at - 8 >= grad && at + 16 <= grad_end;
+          begins[u] = whole ? (uint32_t)reinterpret_cast<uintptr_t>(at) & 15 : 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-          if (i + u < len && mine[r]) term[u][r] = *reinterpret_cast<const Vec<G, VEC>*>(row + r * lanes * (int)(VEC * sizeof(G)));
+          for (int k = 0; k < 8; ++k) raw[u][k] = 0;
+          if (i + u < len && first + lane * 8 < end) {
+            if (whole) {
+              load_shifted(at, raw[u]);
+            } else {
+              G x[8];
+#pragma unroll
+              for (int c = 0; c < 8; ++c) x[c] = first + lane * 8 + c < end ? at[c] : from_float<G>(0.0f);
+              memcpy(raw[u], x, sizeof(x));
+            }
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (i + u < len && mine[r]) term[u][r] = *reinterpret_cast<const Vec<G, VEC>*>(row + r * lanes * (int)(VEC * sizeof(G)));
+        }
       }
       Entry ahead[U];                                       // the next positions, while the terms are on their way
 #pragma unroll
@@ -517,16 +542,32 @@ __global__ void __launch_bounds__(kThreads, VEC == 1 || (VEC >= 4 && !ADD) ? 3 :
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (i + u < len) {
+          if constexpr (SHIFTED) {
+            float f[8];
+            to_floats(shifted<G>(raw[u], begins[u]), f);
+            float(&all)[8] = reinterpret_cast<float(&)[8]>(sum);
+            add_floats(all, f);
+          } else {
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            float f[VEC];
-            to_floats(term[u][r], f);
-            add_floats(sum[r], f);
+            for (int r = 0; r < R; ++r) {
+              float f[VEC];
+              to_floats(term[u][r], f);
+              add_floats(sum[r], f);
+            }
           }
           const bool ends = last >> u & 1;
           if (ends || i + u + 1 == len) {
             if (ends && !began_before) {
               O* at = to + (int64_t)e[u].row * out.stride;
+              if constexpr (SHIFTED) {                      // from the columns it added up to those that it writes
+                float* const mine_in = turned + group * width + lane * 8;
+                __syncwarp(near);
+                *reinterpret_cast<float4*>(mine_in) = make_float4(sum[0][0], sum[1][0], sum[2][0], sum[3][0]);
+                *reinterpret_cast<float4*>(mine_in + 4) = make_float4(sum[4][0], sum[5][0], sum[6][0], sum[7][0]);
+                __syncwarp(near);
+#pragma unroll
+                for (int r = 0; r < R; ++r) sum[r][0] = turned[group * width + lane + r * lanes];
+              }
 #pragma unroll
               for (int r = 0; r < R; ++r) {
                 float f[VEC];
@@ -535,11 +576,11 @@ __global__ void __launch_bounds__(kThreads, VEC == 1 || (VEC >= 4 && !ADD) ? 3 :
                 if (mine[r]) *reinterpret_cast<Vec<O, VEC>*>(at + r * lanes * VEC) = from_floats<O>(f);
               }
             } else {
-              float* keep = piece + (group * 2 + (began_before ? 0 : 1)) * width + lane * VEC;
+              float* keep = piece + (group * 2 + (began_before ? 0 : 1)) * width + (SHIFTED ? lane * 8 : lane * VEC);
 #pragma unroll
               for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) keep[r * lanes * VEC + c] = sum[r][c];
+                for (int c = 0; c < VEC; ++c) keep[SHIFTED ? r : r * lanes * VEC + c] = sum[r][c];
               }
               if (began_before) front_row = e[u].row; else end_row = e[u].row;
             }

@@ -215,3 +215,19 @@ def test_a_table_and_a_vocabulary_trained_served_and_scored():
     v, f = values(packed.q, packed.scales, 32, cfg.dim)
     assert bool((packed.rows(at[:5]).double() == (v * f)[at[:5]].float().double()).all())
     table.close()
+
+
+def test_a_table_without_rows_exports_none():
+    table = mb.MonoTable(1024, 16, 2, 0)
+    ids, packed = table.export_packed(group=128)
+    assert ids.numel() == 0 and len(packed) == 0
+    assert packed.scores(randn(2, 16)).shape == (2, 0)
+    assert bool((packed.rows(torch.arange(5, device="cuda")) == 0).all())
+    # tracked, but below the threshold
+    one = torch.arange(1, 9, device="cuda")
+    table.apply_grads(one, torch.arange(9, device="cuda"), torch.ones((8, 16), device="cuda"), 1)
+    assert table.export_packed()[0].numel() == 0
+    table.apply_grads(one[:3], torch.arange(4, device="cuda"), torch.ones((3, 16), device="cuda"), 2)
+    ids, packed = table.export_packed()
+    assert ids.tolist() == [1, 2, 3] and len(packed) == 3
+    table.close()
