@@ -128,6 +128,38 @@ __device__ __forceinline__ void add_floats(float (&sum)[N], const float (&x)[N])
   }
 }
 
+// x *= by, and x += by
+template <int N>
+__device__ __forceinline__ void scale_floats(float (&x)[N], float by) {
+  if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2)
+      asm("{.reg .b64 a, b; mov.b64 a, {%0, %1}; mov.b64 b, {%2, %2}; mul.rn.f32x2 a, a, b; mov.b64 {%0, %1}, a;}" : "+f"(x[k]), "+f"(x[k + 1]) : "f"(by));
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] *= by;
+  }
+}
+template <int N>
+__device__ __forceinline__ void move_floats(float (&x)[N], float by) {
+  float b[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) b[k] = by;
+  add_floats(x, b);
+}
+
+// (w & mask) | bits in one instruction: with both constants written out the compiler makes two
+__device__ __forceinline__ uint32_t place(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+__device__ __forceinline__ uint32_t kept(uint32_t constant) {
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(constant));
+  return r;
+}
+
 constexpr uint32_t kNoToken = 0xFFFFFFFFu;
 constexpr int64_t kMaxOperatorRows = 0x7FFFFFFEll;      // of a matrix, and tokens of a call
 

@@ -88,31 +88,35 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
   const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes;
   const int64_t row0 = (int64_t)blockIdx.x * groups * ROWS + threadIdx.x / lanes;
   const int words = (p.cols + 7) / 8, w0 = blockIdx.y * lanes * PIECES + lane;
-  uint32_t t[ROWS], q[kMoves] = {};
-  float s[kMoves] = {};
+  uint32_t t[ROWS], q[kMoves];
+  float s[kMoves];
   tokens.rows(row0, groups, t);
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
     const uint32_t row = t[k / PIECES];
     const int w = w0 + (k % PIECES) * lanes;
+    q[k] = 0x88888888u;                                       // (zeros)
+    s[k] = 0.0f;
     if (row != kNoToken && w < words) {
       q[k] = __ldg(reinterpret_cast<const uint32_t*>(p.q + row * p.q_stride) + w);
       s[k] = to_float(static_cast<const S*>(p.scales)[row * p.scale_stride + (w >> group_shift)]);
     }
   }
-  const auto value = [&](bool there, uint32_t nibble, float by) {      // (2^23 + q, less 2^23 + 8)
-    return there ? scale * ((__uint_as_float(0x4B000000u | nibble) - 8388616.0f) * by) : 0.0f;
-  };
+  // q as the lowest bits of 2^23, less 2^23 + 8; without a row all factors are 0
+  const uint32_t mask = 15u, bits = kept(0x4B000000u);
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
     const int64_t i = row0 + (k / PIECES) * groups;
     const int w = w0 + (k % PIECES) * lanes;
-    const bool there = t[k / PIECES] != kNoToken;
+    const float by = t[k / PIECES] != kNoToken ? scale : 0.0f;
+    float f[8];
     if constexpr (ALIGNED) {
       if (i >= tokens.n || w >= words) continue;
-      float f[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) f[c] = value(there, q[k] >> (4 * c) & 15, s[k]);
+      for (int c = 0; c < 8; ++c) f[c] = __uint_as_float(place(q[k] >> (4 * c), mask, bits));
+      move_floats(f, -8388616.0f);
+      scale_floats(f, s[k]);
+      scale_floats(f, by);
       *reinterpret_cast<Vec<O, 8>*>(out + i * out_stride + (int64_t)w * 8) = from_floats<O>(f);
     } else {
       // one column a thread and store, so that neighbours write neighbours: the words are passed round
@@ -122,8 +126,9 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
       for (int c = 0; c < 8; ++c) {
         const int at = c * near + in;                        // among the columns of the threads near by
         const uint32_t word = __shfl_sync(0xFFFFFFFFu, q[k], at / 8, near);
-        const float by = __shfl_sync(0xFFFFFFFFu, s[k], at / 8, near);
-        if (i < tokens.n && (w - in) * 8 + at < p.cols) to[at] = from_float<O>(value(there, word >> (4 * (at % 8)) & 15, by));
+        const float factor = __shfl_sync(0xFFFFFFFFu, s[k], at / 8, near);
+        const float y = by * ((__uint_as_float(place(word >> (4 * (at % 8)), mask, bits)) - 8388616.0f) * factor);
+        if (i < tokens.n && (w - in) * 8 + at < p.cols) to[at] = from_float<O>(y);
       }
     }
   }
@@ -169,11 +174,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 __device__ __forceinline__ uint32_t weights(uint32_t q, uint32_t by) {
   uint32_t r;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(q), "r"(by), "r"(0xA000A000u));
-  return r;
-}
-__device__ __forceinline__ uint32_t kept(uint32_t constant) {
-  uint32_t r;
-  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(constant));
   return r;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127

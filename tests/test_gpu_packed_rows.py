@@ -100,6 +100,7 @@ def test_packed_rows(cols, group):
         tol = want.abs() * (torch.finfo(o).eps / 2 + 2.0 ** -22) + SUBNORMAL[o] / 2
         assert bool(((out[:n].double() - want).abs() <= tol).all())
         assert bool((out[n:] == 7).all())
+        assert not bool(torch.signbit(out[:n][~there]).any())
 
 
 def test_packed_rows_with_strides_and_behind_the_32nd_bit():

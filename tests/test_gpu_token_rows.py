@@ -53,6 +53,19 @@ def check_rows(got, want):
     assert bool((got[want == 0] == 0).all())
 
 
+def test_no_row_is_zeros_whatever_the_factor():
+    weight = randn(40, 33, dtype=BF16)
+    q, scales = torch.full((40, 32), 0x12, dtype=torch.uint8, device="cuda"), torch.full((40, 2), -0.5, device="cuda")
+    tokens = torch.tensor([-1, 40, 3, 7], device="cuda")
+    for scale in (-1.0, float("inf"), float("nan")):
+        for cols in (33, 32):
+            out = torch.full((4, cols), 5.0, device="cuda")
+            mb.mono_token_rows(weight[:, :cols], tokens, out, scale=scale, padding=7)
+            assert bool((out[[0, 1, 3]] == 0).all()) and not bool(torch.signbit(out[[0, 1, 3]]).any())
+            mb.mono_packed_token_rows(q, scales, 32, tokens, out, scale=scale, padding=7)
+            assert bool((out[[0, 1, 3]] == 0).all()) and not bool(torch.signbit(out[[0, 1, 3]]).any())
+
+
 def grad64(grad, tokens, vocab, scale, padding):
     t = tokens.reshape(-1).long()
     there = (t >= 0) & (t < vocab) & (t != padding)
