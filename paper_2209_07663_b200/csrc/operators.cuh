@@ -92,7 +92,7 @@ __device__ __forceinline__ void load_shifted(const T* from, uint32_t (&w)[2 * si
   constexpr int N = sizeof(T) / 2 + 1;
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const uint4 x = __ldg(at + k);
+    const uint4 x = at[k];
     w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
   }
 }
@@ -181,10 +181,10 @@ struct TokenList {
     int64_t t[K];
     if (wide) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? __ldg(static_cast<const long long*>(data) + first + k * step) : -1;
+      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? static_cast<const long long*>(data)[first + k * step] : -1;
     } else {
 #pragma unroll
-      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? __ldg(static_cast<const int*>(data) + first + k * step) : -1;
+      for (int k = 0; k < K; ++k) t[k] = first + k * step < n ? static_cast<const int*>(data)[first + k * step] : -1;
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) row[k] = row_of(t[k]);

@@ -34,7 +34,7 @@ inline PackedView view(const mono_packed_t& p) {
 // Packing: 16 threads a group of columns, group / 16 neighbouring columns each, so that every thread writes whole bytes.
 // ---------------------------------------------------------------------------
 template <typename W, typename S, int GROUP>
-__global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* __restrict__ rows, int64_t stride, PackedView p) {
+__global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* rows, int64_t stride, PackedView p) {
   after_previous_kernel();
   constexpr int N = GROUP / 16;
   const int lane = threadIdx.x % 16;
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
     q[k] = 0x88888888u;                                       // (zeros)
     s[k] = 0.0f;
     if (row != kNoToken && w < words) {
-      q[k] = __ldg(reinterpret_cast<const uint32_t*>(p.q + row * p.q_stride) + w);
+      q[k] = reinterpret_cast<const uint32_t*>(p.q + row * p.q_stride)[w];
       s[k] = to_float(static_cast<const S*>(p.scales)[row * p.scale_stride + (w >> group_shift)]);
     }
   }
@@ -190,7 +190,7 @@ template <int BYTES> struct alignas(BYTES) Words { uint32_t w[BYTES / 4]; };
 // pairs of columns: the powers of two; the sums of the warps, [warps][32][8 * NT].  `columns` operands:
 // vectors, or the parts of vectors.
 template <typename X, typename S, int GROUP, int NT>
-__global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(PackedView p, const X* __restrict__ x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
+__global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(PackedView p, const X* x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
                                                                int64_t out_stride, int split, int64_t tiles) {
   after_previous_kernel();
   constexpr int PARTS = PartsOf<X>::value;

@@ -18,7 +18,7 @@ constexpr int kThreads = 256;
 constexpr int kMoves = 4;                                  // of 4 or 8 columns
 
 template <typename W, typename O, int VEC, int ROWS, int MOVES>
-__global__ void __launch_bounds__(kThreads) token_rows_kernel(const W* __restrict__ weight, int64_t weight_stride, TokenList tokens, float scale,
+__global__ void __launch_bounds__(kThreads) token_rows_kernel(const W* weight, int64_t weight_stride, TokenList tokens, float scale,
                                                               O* __restrict__ out, int64_t out_stride, int vectors, int lanes) {
   after_previous_kernel();
   constexpr int PIECES = MOVES / ROWS;
@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads) token_rows_kernel(const W* __restric
 // ones: with moves of one column 65536 rows of 1023 bf16 columns took 132 us, with these 67 us (1024 columns: 27).  (With moves of two columns or
 // of one fp32 column they are no faster: 130 bf16 columns 9.5 us against 16.6, 1023 fp32 ones 84 against 89.)
 template <typename W, typename O, int ROWS>
-__global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* __restrict__ weight, int64_t weight_stride, TokenList tokens, float scale,
+__global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* weight, int64_t weight_stride, TokenList tokens, float scale,
                                                                       O* __restrict__ out, int64_t out_stride, int cols, int lanes) {
   after_previous_kernel();
   constexpr int PIECES = kMoves / ROWS;
@@ -210,7 +210,7 @@ struct Keys {
     if (entries) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const uint2 x = first + k * step < tokens.n ? __ldg(reinterpret_cast<const uint2*>(entries) + first + k * step) : make_uint2(kBehind, 0);
+        const uint2 x = first + k * step < tokens.n ? reinterpret_cast<const uint2*>(entries)[first + k * step] : make_uint2(kBehind, 0);
         e[k] = {x.x, x.y};
       }
       return;
@@ -236,8 +236,10 @@ __device__ __forceinline__ uint32_t count_before(const uint32_t* keys, int from,
   return n;
 }
 
-// Lets the launch of the kernel behind this one begin; it waits for this one's end itself (after_previous_kernel).  The kernels of a
+// Lets the launch of the call's next kernel begin; it waits for this one's end itself (after_previous_kernel).  The kernels of a
 // gradient are short and leave SMs free (with it and few keys a thread in the sort, 16384 tokens of 1024 columns went from 40 to 34 us).
+// What such a kernel reads may have been written during its lifetime: its inputs are read through the coherent path (no __ldg, no
+// const __restrict__).  A call's last kernel does not let anyone begin.
 __device__ __forceinline__ void release_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // 32 tokens a block; each warp counts over its share of all tokens.
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, i
 }
 
 // counts summed up over kCoarse tiles each
-__global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t* __restrict__ counts, int64_t tiles, uint32_t* __restrict__ coarse) {
+__global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t* counts, int64_t tiles, uint32_t* __restrict__ coarse) {
   after_previous_kernel();
   const int64_t first = (int64_t)blockIdx.x * kCoarse, last = first + kCoarse < tiles ? first + kCoarse : tiles;
   uint32_t sum = 0;
@@ -308,8 +310,8 @@ __global__ void __launch_bounds__(kSortThreads) sum_counts_kernel(const uint32_t
 // A key goes behind the keys of lower digits of all tiles, those of its digit in earlier tiles, in earlier warps of its tile (warp w has the
 // tile's keys [w * 32 * KEYS, (w + 1) * 32 * KEYS)), in earlier rounds of 32 keys, and at lower lanes.
 template <int KEYS>
-__global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, int64_t n, int shift, int bits, const uint32_t* __restrict__ counts, int64_t tiles,
-                                                                    const uint32_t* __restrict__ coarse, Entry* __restrict__ sorted, uint8_t* marks, Zeros zeros) {
+__global__ void __launch_bounds__(kSortThreads) scatter_keys_kernel(Keys keys, int64_t n, int shift, int bits, const uint32_t* counts, int64_t tiles,
+                                                                    const uint32_t* coarse, Entry* __restrict__ sorted, uint8_t* marks, Zeros zeros) {
   after_previous_kernel();
   release_next_kernel();
   if (zeros.here()) { zeros.fill(); return; }
@@ -421,10 +423,10 @@ struct GradOut {
 // blockIdx.x: runs of `run` positions, one for each group of `lanes` threads; blockIdx.y: part_vectors vectors of VEC columns.
 // Without `sorted` (at most kSmallTokens tokens) every block sorts all tokens itself.
 template <typename G, typename O, int VEC, bool ADD>
-__global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) == 2) ? (ADD ? 2 : 3) : VEC == 1 ? 3 : 2) sum_rows_kernel(const G* __restrict__ grad, uint32_t grad_stride, TokenList tokens, const Entry* __restrict__ sorted,
-                                                                                       int run, GradOut<O> out, int part_vectors, int lanes) {
+__global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) == 2) ? (ADD ? 2 : 3) : VEC == 1 ? 3 : 2) sum_rows_kernel(const G* grad, uint32_t grad_stride, TokenList tokens, const Entry* sorted,
+                                                                                       int run, GradOut<O> out, int part_vectors, int lanes, bool joined) {
   after_previous_kernel();
-  release_next_kernel();
+  if (joined) release_next_kernel();
   constexpr int R = kLaneColumns / VEC;
   // Rows of 16-bit elements that begin anywhere: a thread has 8 neighbouring columns of the terms, from the aligned words that hold them, and what
   // it writes passes through shared memory, so that neighbours write neighbours.
@@ -651,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) =
 // A row that begins in block blockIdx.x of the sums (of `positions` sorted positions) and goes on behind it: its partial sums, in order.
 // A thread has VEC columns.
 template <typename O, int VEC>
-__global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* __restrict__ sorted, int64_t n, int positions, bool add, GradOut<O> out) {
+__global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* sorted, int64_t n, int positions, bool add, GradOut<O> out) {
   after_previous_kernel();
   constexpr int U = 16;
   const int64_t b = blockIdx.x, p0 = b * positions, p1 = p0 + positions;
@@ -841,11 +843,12 @@ int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale,
       place = place == w.a ? w.b : w.a;
     }
   }
+  const bool joins = sums.blocks >= 2 && n > kSmallTokens;
   const auto sum = [&](auto* kernel) {
-    return launch_operator(kernel, sum_grid, kThreads, 0, s, from, (uint32_t)(grad.stride * (int64_t)sizeof(G)), tokens, sorted, sums.run, to, sums.part_vectors, sums.lanes);
+    return launch_operator(kernel, sum_grid, kThreads, 0, s, from, (uint32_t)(grad.stride * (int64_t)sizeof(G)), tokens, sorted, sums.run, to, sums.part_vectors, sums.lanes, joins);
   };
   rc = accumulate ? sum(sum_rows_kernel<G, O, VEC, true>) : sum(sum_rows_kernel<G, O, VEC, false>);
-  if (rc != MONO_OK || sums.blocks < 2 || n <= kSmallTokens) return rc;
+  if (rc != MONO_OK || !joins) return rc;
   constexpr int JOINED = std::min(4, VEC);
   const int joined = cols / JOINED, threads = joined >= kThreads ? kThreads : (joined + 31) / 32 * 32;
   return launch_operator(join_rows_kernel<O, JOINED>, dim3((unsigned)(sums.blocks - 1), (unsigned)((joined + threads - 1) / threads)), threads, 0, s, sorted, n, sums.run * sums.groups,
