@@ -31,46 +31,62 @@ inline PackedView view(const mono_packed_t& p) {
 }
 
 // ---------------------------------------------------------------------------
-// Packing: 16 threads a group of columns, group / 16 neighbouring columns each, so that every thread writes whole bytes.
+// Packing: 8 threads a group of columns, group / 8 neighbouring columns each, so that every thread writes whole bytes.  A block has the groups of
+// blockIdx.y's share of kPackGroups / block_groups rows.  (131072 rows of 1024 fp32 columns: 172 us, of which the bytes are 93; what a thread does once for its columns
+// is the rest.  With half as many columns each, single columns read and a 64-bit division to find them it took 288.)
 // ---------------------------------------------------------------------------
-template <typename W, typename S, int GROUP>
-__global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* rows, int64_t stride, PackedView p) {
+constexpr int kPackThreads = 8, kPackGroups = kThreads / kPackThreads;
+
+template <typename W, typename S, int GROUP, bool VECTORS>
+__global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* rows, int64_t stride, PackedView p, int block_groups) {
   after_previous_kernel();
-  constexpr int N = GROUP / 16;
-  const int lane = threadIdx.x % 16;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16;
-  const int64_t row = item / p.groups;
-  if (row >= p.rows) return;                                // (all 16 threads of a group)
-  const unsigned members = 0xFFFFu << (threadIdx.x & 16);
-  const int g = (int)(item % p.groups), c0 = g * GROUP + lane * N;
+  constexpr int N = GROUP / kPackThreads, V = N < 8 ? N : 8;
+  const int lane = threadIdx.x % kPackThreads, sub = threadIdx.x / kPackThreads;
+  const int64_t row = (int64_t)blockIdx.x * (kPackGroups / block_groups) + sub / block_groups;
+  const int g = blockIdx.y * block_groups + sub % block_groups, c0 = g * GROUP + lane * N;
+  if (row >= p.rows || g >= p.groups) return;               // (all threads of a group)
+  const unsigned members = 0xFFu << (threadIdx.x & 24);
+  const W* const from = rows + row * stride + c0;
   float w[N];
+  if (VECTORS && c0 + N <= p.cols) {
+#pragma unroll
+    for (int i = 0; i < N; i += V) to_floats(*reinterpret_cast<const Vec<W, V>*>(from + i), reinterpret_cast<float(&)[V]>(w[i]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = c0 + i < p.cols ? to_float(from[i]) : 0.0f;
+  }
   float most = 0.0f;
   bool nan = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    w[i] = c0 + i < p.cols ? to_float(rows[row * stride + c0 + i]) : 0.0f;
     most = fmaxf(most, fabsf(w[i]));                        // (fmaxf passes over a NaN)
     nan |= w[i] != w[i];
   }
 #pragma unroll
-  for (int s = 8; s > 0; s /= 2) {
-    most = fmaxf(most, __shfl_xor_sync(members, most, s));
-    nan |= __shfl_xor_sync(members, (int)nan, s) != 0;
-  }
+  for (int s = kPackThreads / 2; s > 0; s /= 2) most = fmaxf(most, __shfl_xor_sync(members, most, s));
+  nan = __any_sync(members, nan);
   const S stored = from_float<S>(nan ? __int_as_float(0x7FC00000) : __fdiv_rn(most, 7.0f));
   const float scale = to_float(stored);
   const bool usable = scale > 0.0f && scale <= 3.402823466e38f;
-  const int64_t padded = (int64_t)((p.cols + 31) / 32) * 16;      // bytes of a row that are written
+  // The quotient rounded to a whole number.  By the reciprocal it is off by less than 2^-22 of itself, which is below 2^-18 for the numbers up to 16
+  // (beyond, it is held to 7 either way): only where it is that near to a half the quotient itself has to say.
+  const float inverse = __fdiv_rn(1.0f, scale);
+  const bool exactly = !(inverse <= 3.402823466e38f);       // (a scale so small that it has none)
+  uint64_t bytes = 0;
 #pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    int q[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float r = usable ? fminf(fmaxf(rintf(__fdiv_rn(w[i + j], scale)), -7.0f), 7.0f) : 0.0f;
-      q[j] = (int)r + 8;
-    }
-    const int64_t byte = (c0 + i) / 2;
-    if (byte < padded) p.q[row * p.q_stride + byte] = (uint8_t)(q[0] | q[1] << 4);
+  for (int i = 0; i < N; ++i) {
+    const float quotient = w[i] * inverse;
+    float r = rintf(quotient);
+    if (exactly || fabsf(fabsf(quotient - r) - 0.5f) < 1.0f / 65536.0f) r = rintf(__fdiv_rn(w[i], scale));
+    r = usable ? fminf(fmaxf(r, -7.0f), 7.0f) : 0.0f;
+    bytes |= (uint64_t)(uint32_t)((int)r + 8) << (4 * i);
+  }
+  const int at = c0 / 2, padded = (p.cols + 31) / 32 * 16;  // bytes of a row that are written
+  uint8_t* const to = p.q + row * p.q_stride + at;
+  if (at < padded) {                                        // (a multiple of 16: all of a thread's bytes or none)
+    if constexpr (N == 16) *reinterpret_cast<uint64_t*>(to) = bytes;
+    else if constexpr (N == 8) *reinterpret_cast<uint32_t*>(to) = (uint32_t)bytes;
+    else *reinterpret_cast<uint16_t*>(to) = (uint16_t)bytes;
   }
   if (lane == 0) static_cast<S*>(p.scales)[row * p.scale_stride + g] = stored;
 }
@@ -485,14 +501,21 @@ int mono_pack_rows(const mono_matrix_t* rows, const mono_packed_t* packed, void*
   if (!matrix_ok(rows, false) || !packed_ok(packed) || rows->rows != packed->rows || rows->cols != packed->cols) return MONO_ERR_ARG;
   if (packed->rows == 0) return MONO_OK;
   const PackedView p = view(*packed);
-  const int64_t blocks = (p.rows * p.groups + kThreads / 16 - 1) / (kThreads / 16);
-  if (blocks > INT_MAX) return MONO_ERR_LIMIT;
+  int block_groups = 1;
+  while (block_groups < kPackGroups && block_groups < p.groups) block_groups *= 2;
+  const int64_t block_rows = kPackGroups / block_groups;
+  const dim3 grid((unsigned)((p.rows + block_rows - 1) / block_rows), (unsigned)((p.groups + block_groups - 1) / block_groups));
+  const int vectors = vector_of({rows->data, rows->rows, (p.cols + 7) / 8 * 8, rows->stride, rows->type, 0});      // (of a row's whole vectors)
   return with_type(rows->type, [&](auto w) {
     return with_type(packed->scale_type, [&](auto s) {
       return with_group(packed->group, [&](auto g) {
         using W = decltype(w);
-        return launch_operator(pack_rows_kernel<W, decltype(s), decltype(g)::value>, dim3((unsigned)blocks), kThreads, 0, static_cast<cudaStream_t>(cuda_stream),
-                               static_cast<const W*>(rows->data), rows->stride, p);
+        using S = decltype(s);
+        constexpr int GROUP = decltype(g)::value;
+        const auto launch = [&](auto* kernel) {
+          return launch_operator(kernel, grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const W*>(rows->data), rows->stride, p, block_groups);
+        };
+        return vectors >= std::min(8, GROUP / kPackThreads) ? launch(pack_rows_kernel<W, S, GROUP, true>) : launch(pack_rows_kernel<W, S, GROUP, false>);
       });
     });
   });

@@ -65,6 +65,28 @@ def test_packing(cols, group):
         assert torch.equal(q[:, :padded], halves[:, 0::2] | halves[:, 1::2] << 4)
 
 
+@pytest.mark.parametrize("scales", TYPES)
+def test_packing_rounds_the_quotient_and_not_something_near_it(scales):
+    # quotients around every half between -8 and 8: the numbers next to half a scale on both sides
+    for top in (7.0, 1.0, 0.1, 3e-5, 1e-38, 1e-44, 5e37):
+        rows = torch.zeros((64, 128), device="cuda")
+        rows[:, 0] = top
+        scale = (rows[:, :1] / torch.tensor(7.0, device="cuda")).to(scales).float()
+        halves = (torch.arange(-8, 8, device="cuda") + 0.5).repeat_interleave(4)[None, :] * scale
+        near = halves.clone()
+        for k in range(64):
+            x = near[k].view(torch.int32) + (k % 9 - 4)     # up to four numbers further on
+            rows[k, 32:96] = x.view(torch.float32)
+        rows = torch.where(rows.abs() <= top, rows, 0.0)
+        rows[:, 0] = top
+        q, s = torch.empty((64, 64), dtype=torch.uint8, device="cuda"), torch.empty((64, 1), dtype=scales, device="cuda")
+        mb.mono_pack_rows(rows, q, s, 128)
+        by = s.float()
+        usable = (by > 0) & torch.isfinite(by)
+        got = torch.stack((q & 15, q >> 4), -1).flatten(1)
+        assert torch.equal(got, (torch.where(usable, torch.round(rows / torch.where(usable, by, 1.0)).clamp(-7, 7), 0.0) + 8).to(torch.uint8)), top
+
+
 def test_packing_what_is_not_finite_or_too_large_or_too_small():
     rows = randn(6, 64)
     rows[0, 3], rows[1, 40], rows[2, 1] = float("nan"), float("inf"), float("-inf")
