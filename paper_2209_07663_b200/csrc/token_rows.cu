@@ -151,7 +151,7 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
 // use a few SMs for a few microseconds: of all rows, or, where the sort has several passes, of those that the first pass did not mark.
 //
 // Measured: 262144 tokens, 1024 bf16 columns, fp32 gradient of 131072 rows: 224 us, of which the sums are 129 (660 MB, 5.1 TB/s), the sort with the
-// zeros 85 and the joins 9; 4096 tokens of 1024 columns, bf16 gradient of 32000 rows 25 us; 77 tokens of 64 columns 4.9 us.
+// zeros 85 and the joins 9; 4096 tokens of 1024 columns, bf16 gradient of 32000 rows 24 us; 77 tokens of 64 columns 4.9 us.
 // ---------------------------------------------------------------------------
 constexpr int64_t kSmallTokens = 512;
 constexpr int kSmallRun = 2;                                // their positions of a group
@@ -246,33 +246,47 @@ __device__ __forceinline__ uint32_t count_before(const uint32_t* keys, int from,
 // const __restrict__).  A call's last kernel does not let anyone begin.
 __device__ __forceinline__ void release_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// 32 tokens a block; each warp counts over its share of all tokens.
+// 32 tokens a block; each warp counts over its share of all tokens, four at a time: those in front of the block's, up to the key, those behind
+// them, below it.
 __global__ void __launch_bounds__(kThreads) rank_tokens_kernel(TokenList tokens, Entry* __restrict__ sorted, Zeros zeros) {
   after_previous_kernel();
   release_next_kernel();
   if (zeros.here()) { zeros.fill(); return; }
   constexpr int kWarps = kThreads / 32;
-  __shared__ uint32_t keys[kRankTokens];
+  __shared__ __align__(16) uint32_t keys[kRankTokens];
   __shared__ uint32_t counts[kWarps][32];
   const Keys all{tokens, nullptr};
-  const int n = (int)tokens.n, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kThreads) {
+  const int n = (int)tokens.n, padded = (n + 31) / 32 * 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int i0 = threadIdx.x; i0 < padded; i0 += 8 * kThreads) {
     Entry e[8];
     all.load(i0, kThreads, e);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (i0 + k * kThreads < n) keys[i0 + k * kThreads] = e[k].row;
+      if (i0 + k * kThreads < padded) keys[i0 + k * kThreads] = e[k].row;        // (kBehind behind the last one: below none)
   }
   __syncthreads();
-  const int mine = blockIdx.x * 32 + lane, share = (n + kWarps - 1) / kWarps;
-  const int from = min(warp * share, n), to = min(from + share, n);
-  counts[warp][lane] = mine < n ? count_before(keys, from, to, keys[mine], mine) : 0;
+  const int first = blockIdx.x * 32, mine = first + lane, share = (padded / 32 + kWarps - 1) / kWarps * 32;
+  const int from = min(warp * share, padded), to = min(from + share, padded);
+  const uint32_t key = keys[mine];
+  uint32_t before = 0;
+#pragma unroll 4
+  for (int j = from; j < min(to, first); j += 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(keys + j);
+    before += (x.x <= key) + (x.y <= key) + (x.z <= key) + (x.w <= key);
+  }
+#pragma unroll 4
+  for (int j = max(from, first + 32); j < to; j += 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(keys + j);
+    before += (x.x < key) + (x.y < key) + (x.z < key) + (x.w < key);
+  }
+  if (from <= first && first < to) before += count_before(keys, first, first + 32, key, mine);
+  counts[warp][lane] = before;
   __syncthreads();
   if (warp != 0 || mine >= n) return;
   uint32_t place = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) place += counts[w][lane];
-  sorted[place] = {keys[mine], (uint32_t)mine};
+  sorted[place] = {key, (uint32_t)mine};
   if (mine == 0) sorted[n] = {kBehind, 0};
 }
 
@@ -804,7 +818,7 @@ int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale,
     zeros.begin = vocab * k / shares;
     zeros.end = vocab * (k + 1) / shares;
     zeros.first = fills ? (unsigned)blocks : UINT_MAX;
-    *grid = dim3((unsigned)blocks + (fills ? kZeroBlocks : 0));
+    *grid = dim3((unsigned)blocks + (fills ? (n <= kRankTokens ? 2 : 1) * kZeroBlocks : 0));        // (of half as many threads)
     return zeros;
   };
   const SumPlan sums = plan_sums(n, cols / VEC, VEC);
