@@ -532,8 +532,8 @@ int mono_timing_read(mono_table* t, mono_timing_t* host_out, int reset);
  *  - A matrix that is written must not overlap anything else the call is given.  Of a matrix that is read, what lies between
  *    its rows may be read too (and is not used).
  *  - Products and sums are taken in fp32, and what is written is rounded once, to nearest even.
- *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS, strides up to MONO_MAX_STRIDE (a row of
- *    scores has one column per packed row).
+ *  - Limits: rows and tokens up to 2^31 - 2, columns up to MONO_MAX_COLS, strides up to MONO_MAX_STRIDE (but a row
+ *    of scores has one column per packed row, and scores' stride is limited as rows are).
  *  - A token outside [0, vocabulary) has no row: it looks up as zeros and its gradient is dropped, like MONO_RESERVED_ID in
  *    a table.  So does the token `padding` (-1, or any other number outside the vocabulary, for none).
  */
