@@ -206,7 +206,7 @@ __device__ __forceinline__ void store_as(void* to, int type, int64_t i, float y)
 template <int BYTES> struct alignas(BYTES) Words { uint32_t w[BYTES / 4]; };
 
 // Shared memory: the warps' stages, [warps][kStages][32][128 bytes]; the vectors, [words of a quarter row][columns][4 threads][4 pairs]; of each group, [4 * NT]
-// pairs of columns: the powers of two; the sums of the warps, [warps][32][8 * NT].  `columns` operands:
+// pairs of columns: the powers of two that their sums are multiplied by; the sums of the warps, [warps][32][8 * NT].  `columns` operands:
 // vectors, or the parts of vectors.
 template <typename X, typename S, int GROUP, int NT>
 __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(PackedView p, const X* x, int64_t x_stride, int vectors, void* __restrict__ out, int out_type,
@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
         for (int k = 0; k < 4; ++k) e8[2 * k] = part[j][k], e8[2 * k + 1] = part[j][k + 4];
         memcpy(&operands[(word * columns + col) * 4 + in / (GROUP / 4)], e8, sizeof(uint4));
         if (in == 0) {
-          reinterpret_cast<float*>(&groups[group * 4 * NT + col / 2])[col % 2] = power_of_two(e);
+          // (exact, a subnormal for e < -122; taken off the scale or off the product instead, scales would lose bits and sums overflow that fp32 has room for)
+          reinterpret_cast<float*>(&groups[group * 4 * NT + col / 2])[col % 2] = 0.0625f * power_of_two(e);
         }
       }
     }
@@ -395,10 +396,10 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
             }
           }
         }
-        // the weights' 2^-10, the vectors' power of two: of its exponent, 14 is in the operands
+        // of_group: the vectors' power of two, less the 14 of its exponent that are in the operands and the weights' 2^-10
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-          const float f = 0.0625f * (U == 1 ? to_float(own[j][0]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4)));
+          const float f = U == 1 ? to_float(own[j][0]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             total[j / 2][nt][j % 2 * 2] += f * (of_group[nt].x * sum[j / 2][nt][j % 2 * 2]);

@@ -213,6 +213,39 @@ def test_scores_of_large_and_small_fp32_vectors():
         check_scores(out, q, scales, 32, x)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_scores_whose_group_sums_are_near_the_largest_numbers(t, group):
+    # every group's sum is finite in fp32: at most 8 * 32 * 2^119 = 8 * 128 * 2^117 = 2^127
+    cols, top = 2 * group + 3, 118 if group == 32 else 116
+    q, scales = packed(90, cols, group)
+    q[3:6] = 0xFF                                          # every weight 7
+    x = ((torch.rand((3, cols), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) + 1) * 2.0 ** top).to(t)
+    x[1, ::2] *= -1
+    # one element at the type's end, its weight 1 in row 7, -1 in row 8 and 0 elsewhere
+    q[:, 0] = q[:, 0] & 0xF0 | 8
+    q[7, 0], q[8, 0] = q[7, 0] & 0xF0 | 9, q[8, 0] & 0xF0 | 7
+    x[2] = 0
+    x[2, 0] = torch.finfo(t).max
+    out = torch.empty((3, 90), device="cuda")
+    mb.mono_packed_scores(q, scales, group, x, out)
+    assert bool(torch.isfinite(out).all())
+    check_scores(out, q, scales, group, x)
+
+
+@pytest.mark.parametrize("s", [F32, BF16])
+def test_scores_of_rows_with_subnormal_scales(s):
+    least = SUBNORMAL[s]
+    q, _ = packed(60, 96, 32)
+    scales = (torch.arange(1, 181, device="cuda").view(60, 3).double() * least).to(s)
+    assert bool((scales.double() % least == 0).all()) and float(scales.double().min()) == least
+    for t in (F32, BF16):                                  # (large enough that the scores are normal numbers)
+        x = randn(2, 96, dtype=t, scale=2.0 ** 72)
+        out = torch.empty((2, 60), device="cuda")
+        mb.mono_packed_scores(q, scales, 32, x, out)
+        check_scores(out, q, scales, 32, x)
+
+
 def test_a_vector_alone_and_no_vectors():
     q, scales = packed(40, 64, 32)
     x, out = randn(64), torch.empty(40, device="cuda")
