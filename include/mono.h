@@ -610,7 +610,8 @@ int mono_packed_token_rows(const mono_packed_t* packed, const void* tokens, int3
  * Scores of every packed row against a few vectors (a user's vector against all candidates; the output layer that shares
  * the input layer's matrix):  out[m, v] = sum over c of x[m, c] * value(v, c), taken as
  *     sum over groups of  scale(v, group) * (sum over the group's c of x[m, c] * (q(v, c) - 8)),
- * all sums in fp32 and, but for elements of x below 2^-36 of the largest of their group, no product rounded.
+ * all sums in fp32 and no product rounded, x being taken as it is but for elements that are small beside the largest (in size) of
+ * their group: fp32 ones below 2^-38 of it are off by up to 2^-62 of it, bf16 ones below 2^-32 by up to 2^-40; fp16 ones never.
  *  x        [up to MONO_MAX_SCORED, packed->cols]; MONO_ERR_LIMIT for more rows: that is a matrix product
  *  out      [x->rows, packed->rows], any of the types
  * MONO_ERR_LIMIT too for more than MONO_MAX_SCORED_COLS columns.

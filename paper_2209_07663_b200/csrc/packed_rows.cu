@@ -158,9 +158,11 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // the next ones 16 * q * 2^-24, subnormal and exact; times 2^14 or 2^10, less 8 * 2^-10, they are (q - 8) * 2^-10: an AND and
 // a multiply-add for two weights, and a shift for each eight.  (Left subnormal, with the 8 taken off the sums, they took 71 us instead of
 // 75 for 8 vectors against 131072 rows of 4096 columns, and the sums lost three bits.)
-// Vectors become fp16 operands that lose nothing that fp32 sums would keep: those of a group are multiplied by the power of two that takes
-// the largest of them to 2^14 .. 2^15, so that only what is below 2^-36 of it is rounded at all, and fp32 vectors are three operands
-// whose sum they are.  All products are exact, all sums in fp32.
+// Vectors become fp16 operands: those of a group are multiplied by the power of two that takes the largest of them to 2^15 .. 2^16, and an
+// fp32 vector is three operands whose sum it is, the second and third times 2^11 and 2^22, so that each has 11 bits of its own however small
+// an element is beside the others.  With fp16's least number, 2^-24, that leaves fp32 elements as they are down to 2^-38 of the group's largest (below,
+// they are off by at most 2^-62 of it), bf16 ones down to 2^-32 (2^-40), and all fp16 ones.  (A bf16 vector in two operands would have the
+// fp32 one's range for twice the products.)  All products are exact, all sums in fp32.
 //
 // In a product of mma.m16n8k16 the columns are summed over, so any may stand in any place, as long as the vectors' are in the same.
 // So thread t of the four that share a row takes the t-th quarter of a group's bytes as they lie, and what the masks select of a word, columns p
@@ -282,17 +284,18 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
       }
 #pragma unroll
       for (int s = GROUP / 16; s > 0; s /= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, s));
-      const int e = max((int)(most >> 23), 1) - 127;         // of the largest; a subnormal's is that of the smallest normal number
-      const float up0 = power_of_two((14 - e) / 2), up1 = power_of_two(14 - e - (14 - e) / 2);
+      // of the largest's exponent; the least that leaves the third part's factor a normal number, and no element loses by it: 2^-149 is 2^-35 in an operand
+      const int e = max((int)(most >> 23) - 127, -99);
+      const float up = power_of_two(15 - e);
       __half part[PARTS][8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        float left = v[k] * up0 * up1;
+        float left = v[k] * up;
 #pragma unroll
         for (int j = 0; j < PARTS; ++j) {
           // (cut, so that what is left has the same sign and fewer bits; of what is not finite nothing is left)
           part[j][k] = j + 1 < PARTS ? __float2half_rz(left) : __float2half_rn(left);
-          left = fabsf(left) < 65536.0f ? left - __half2float(part[j][k]) : 0.0f;
+          left = fabsf(left) < 65536.0f ? (left - __half2float(part[j][k])) * 2048.0f : 0.0f;
           if (PARTS > 1 && j == 0 && !(fabsf(v[k]) <= 3.402823466e38f)) part[j][k] = __float2half_rn(v[k]);
         }
       }
@@ -306,8 +309,9 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
         for (int k = 0; k < 4; ++k) e8[2 * k] = part[j][k], e8[2 * k + 1] = part[j][k + 4];
         memcpy(&operands[(word * columns + col) * 4 + in / (GROUP / 4)], e8, sizeof(uint4));
         if (in == 0) {
-          // (exact, a subnormal for e < -122; taken off the scale or off the product instead, scales would lose bits and sums overflow that fp32 has room for)
-          reinterpret_cast<float*>(&groups[group * 4 * NT + col / 2])[col % 2] = 0.0625f * power_of_two(e);
+          // what turns the operands' sums into the group's: from -126 to 122.  (Taken off the scale or off the product instead, part of it made sums
+          // overflow that fp32 has room for, and took bits off subnormal scales.)
+          reinterpret_cast<float*>(&groups[group * 4 * NT + col / 2])[col % 2] = power_of_two(e - 5 - 11 * j);
         }
       }
     }
@@ -396,7 +400,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
             }
           }
         }
-        // of_group: the vectors' power of two, less the 14 of its exponent that are in the operands and the weights' 2^-10
+        // of_group: the operands' powers of two and the weights' 2^-10, taken back
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
           const float f = U == 1 ? to_float(own[j][0]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4));

@@ -233,6 +233,53 @@ def test_scores_whose_group_sums_are_near_the_largest_numbers(t, group):
     check_scores(out, q, scales, group, x)
 
 
+def lopsided(cols, group, k, seed=0):
+    """Vectors whose columns of weight 0 (two of every quarter of a group) are 1 and the others 2^-k .. 2^(1-k), and rows for them."""
+    q, scales = packed(50, cols, group, F32, seed=seed)
+    q[:, ::group // 8] = 0x88
+    heavy = torch.arange(cols, device="cuda") // 2 % (group // 8) == 0
+    x = (1 + torch.rand((2, cols), device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))) * 2.0 ** -k
+    x[:, heavy] = 1.0
+    return q, scales, x * torch.where(torch.arange(cols, device="cuda") % 3 == 0, -1, 1)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("t,least", [(F32, 38), (BF16, 32), (F16, 34)])
+def test_scores_of_elements_that_are_small_beside_others_of_their_group(t, least, group):
+    # what the large elements are multiplied by is 0, so the scores are those of the small ones, and their tolerance too
+    for k in range(8, least + 1, 2):
+        q, scales, x = lopsided(2 * group + 5, group, k, seed=k)
+        x = (x * 2.0 ** (15 if t is F16 else -20)).to(t)      # (fp16: down to a few of its least number)
+        out = torch.empty((2, 50), device="cuda")
+        mb.mono_packed_scores(q, scales, group, x, out)
+        check_scores(out, q, scales, group, x)
+
+
+@pytest.mark.parametrize("t,least,lost", [(F32, 38, 62), (BF16, 32, 40)])
+def test_scores_of_elements_that_are_smaller_than_that(t, least, lost):
+    for k in range(least, lost + 6, 2):
+        q, scales, x = lopsided(70, 64, k, seed=k)
+        x = x.to(t)
+        out = torch.empty((2, 50), device="cuda")
+        mb.mono_packed_scores(q, scales, 64, x, out)
+        v, s = values(q, scales, 64, 70)
+        want, size = x.double() @ (v * s).T, x.double().abs() @ (v * s).abs().T
+        # (the last group has one large column and five small ones; what is off by 2^-lost of the largest, 1, is every small column)
+        tol = size * (64 + 2 + 16) * 2.0 ** -23 + (v * s).abs().sum(1) * 2.0 ** -lost
+        assert bool(((out.double() - want).abs() <= tol).all()), k
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("top", [2.0 ** -90, 2.0 ** -100, 2.0 ** -115, 2.0 ** -124, 2.0 ** -126, 2.0 ** -130])
+def test_scores_of_vectors_near_the_smallest_numbers(t, top):
+    q, scales = packed(80, 100, 32, F32)
+    x = (randn(3, 100).clamp(-2, 2).double() * top).to(t)
+    assert bool((x != 0).any())
+    out = torch.empty((3, 80), device="cuda")
+    mb.mono_packed_scores(q, scales * 2.0 ** 70, 32, x, out)      # (normal numbers)
+    check_scores(out, q, scales * 2.0 ** 70, 32, x)
+
+
 @pytest.mark.parametrize("s", [F32, BF16])
 def test_scores_of_rows_with_subnormal_scales(s):
     least = SUBNORMAL[s]
