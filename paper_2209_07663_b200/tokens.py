@@ -83,6 +83,10 @@ class PackedRows:
     def replace(self, at, rows):
         """Pack `rows` in the place of those at `at` (distinct row numbers): what a serving process does with the rows that
         MonoTable.export_touched shipped."""
+        if rows.dim() != 2 or rows.shape[1] != self.cols:
+            raise ValueError(f"rows: a matrix of {self.cols} columns is expected")
+        if at.dim() != 1 or at.shape[0] != rows.shape[0]:
+            raise ValueError("at: a row number for each of the rows is expected")
         p = PackedRows.pack(rows, self.group, self.scales.dtype)
         self.q[:, :p.q.shape[1]].index_copy_(0, at, p.q)
         self.scales[:, :p.scales.shape[1]].index_copy_(0, at, p.scales)

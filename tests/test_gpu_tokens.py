@@ -231,3 +231,20 @@ def test_a_table_without_rows_exports_none():
     ids, packed = table.export_packed()
     assert ids.tolist() == [1, 2, 3] and len(packed) == 3
     table.close()
+
+
+@pytest.mark.parametrize("cols,group,others", [(64, 32, (32, 63, 65, 128)), (40, 32, (8, 33, 41, 64, 72)), (130, 128, (1, 128, 131, 160))])
+def test_rows_of_another_width_replace_none(cols, group, others):
+    packed = PackedRows.pack(randn(10, cols), group)
+    q, scales, at = packed.q.clone(), packed.scales.clone(), torch.tensor([3, 7], device="cuda")
+    for rows, to in [(randn(2, c), at) for c in others] + [(randn(2, cols), at[:1]), (randn(3, cols), at), (randn(2, cols), at[:, None]), (randn(cols), at[:1])]:
+        with pytest.raises(ValueError):
+            packed.replace(to, rows)
+    assert torch.equal(packed.q, q) and torch.equal(packed.scales, scales)
+    new = randn(2, cols, seed=1)
+    packed.replace(at, new)
+    want = PackedRows.pack(new, group)
+    assert torch.equal(packed.q[at], want.q) and torch.equal(packed.scales[at], want.scales)
+    rest = [r for r in range(10) if r not in (3, 7)]
+    assert torch.equal(packed.q[rest], q[rest]) and torch.equal(packed.scales[rest], scales[rest])
+    packed.replace(at[:0], new[:0])
