@@ -81,12 +81,19 @@ class PackedRows:
         return self.q.shape[0]
 
     def replace(self, at, rows):
-        """Pack `rows` in the place of those at `at` (distinct row numbers): what a serving process does with the rows that
-        MonoTable.export_touched shipped."""
+        """Pack `rows` in the place of those at `at`: what a serving process does with the rows that MonoTable.export_touched
+        shipped.  at: int64, distinct row numbers from 0 on, which is checked (and waited for), but not while a CUDA graph is captured."""
         if rows.dim() != 2 or rows.shape[1] != self.cols:
             raise ValueError(f"rows: a matrix of {self.cols} columns is expected")
         if at.dim() != 1 or at.shape[0] != rows.shape[0]:
             raise ValueError("at: a row number for each of the rows is expected")
+        if at.dtype != torch.int64 or at.device != self.q.device:
+            raise ValueError("at: int64 row numbers on the packed rows' device are expected")
+        if at.numel() and not torch.cuda.is_current_stream_capturing():
+            # a number outside would end the context in a device assertion, a repeated one mix one row's columns with another's scales
+            ordered = at.sort().values
+            if bool((ordered[0] < 0) | (ordered[-1] >= len(self)) | (ordered[1:] == ordered[:-1]).any()):
+                raise ValueError(f"at: distinct row numbers below {len(self)} are expected")
         p = PackedRows.pack(rows, self.group, self.scales.dtype)
         self.q[:, :p.q.shape[1]].index_copy_(0, at, p.q)
         self.scales[:, :p.scales.shape[1]].index_copy_(0, at, p.scales)

@@ -248,3 +248,38 @@ def test_rows_of_another_width_replace_none(cols, group, others):
     rest = [r for r in range(10) if r not in (3, 7)]
     assert torch.equal(packed.q[rest], q[rest]) and torch.equal(packed.scales[rest], scales[rest])
     packed.replace(at[:0], new[:0])
+
+
+def test_row_numbers_that_name_no_row_or_one_twice_replace_none():
+    packed = PackedRows.pack(randn(10, 64), 32)
+    q, scales, new = packed.q.clone(), packed.scales.clone(), randn(3, 64, seed=1)
+    for at in ([0, 1, 10], [0, -1, 2], [3, 4, 3], [-1, -1, -1], [2 ** 40, 1, 2], [-2 ** 63, 2 ** 63 - 1, 0]):
+        with pytest.raises(ValueError):
+            packed.replace(torch.tensor(at, device="cuda"), new)
+    for at in (torch.arange(3, device="cuda", dtype=torch.int32), torch.arange(3), torch.zeros(3, device="cuda")):
+        with pytest.raises(ValueError):
+            packed.replace(at, new)
+    with pytest.raises(ValueError):
+        PackedRows.empty(0, 64, 32).replace(torch.zeros(1, dtype=torch.int64, device="cuda"), new[:1])
+    assert torch.equal(packed.q, q) and torch.equal(packed.scales, scales)
+    packed.replace(torch.tensor([9, 0, 5], device="cuda"), new)
+    want = PackedRows.pack(new, 32)
+    assert torch.equal(packed.q[[9, 0, 5]], want.q) and torch.equal(packed.scales[[9, 0, 5]], want.scales)
+
+
+def test_rows_are_replaced_in_a_graph():
+    packed = PackedRows.pack(randn(10, 64), 32)
+    at, new = torch.tensor([4, 2], device="cuda"), randn(2, 64, seed=1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        packed.replace(at, new)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        packed.replace(at, new)
+    at.copy_(torch.tensor([7, 0], device="cuda"))
+    new.copy_(randn(2, 64, seed=2))
+    graph.replay()
+    want = PackedRows.pack(new, 32)
+    assert torch.equal(packed.q[[7, 0]], want.q) and torch.equal(packed.scales[[7, 0]], want.scales)
