@@ -438,7 +438,7 @@ int mono_read_rows(mono_table* t, const uint64_t* ids, int64_t n, float* w, floa
 /*
  * Dump every tracked ID (any order) into caller buffers of max_n entries:
  * ids, count, last_seen, resident, and fp32 [max_n, dim] w / acc (zeros for IDs
- * without a row; w and acc may be NULL).  n_out HOST receives the number
+ * without a row); all but ids may be NULL.  n_out HOST receives the number
  * written.  MONO_ERR_SIZE (and *n_out = needed) if max_n is too small.
  * This is the table's snapshot (Section 2.3) in its simplest form.
  */

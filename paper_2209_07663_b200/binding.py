@@ -496,6 +496,8 @@ class MonoTable:
     ids are passed as int64 or uint64 tensors (the bit pattern is what counts).
     """
 
+    PACK_BYTES = 1 << 28      # of fp32 rows that export_packed has at once
+
     def __init__(self, capacity: int, dim: int, filter_threshold: int, ttl: int, **opt):
         import torch
         self._torch = torch
@@ -606,18 +608,28 @@ class MonoTable:
 
     def export_packed(self, group: int = 64, scale_dtype=None):
         """The rows in 4 bits for a serving process: (int64 tensor of the IDs that own rows, their PackedRows), sorted by
-        the IDs' bits as signed numbers, both on the device."""
+        the IDs' bits as signed numbers, both on the device.  The fp32 rows pass through a buffer of PACK_BYTES: what it takes beside
+        the table are the packed rows and a few copies of the IDs."""
         torch = self._torch
         from .tokens import PackedRows
+        stream = torch.cuda.current_stream()
         n = int(self.status()["n_tracked"]) + 8
         ids = torch.empty(n, dtype=torch.int64, device="cuda")
         resident = torch.empty(n, dtype=torch.uint8, device="cuda")
-        w = torch.empty((n, self.dim), dtype=torch.float32, device="cuda")
-        count, seen = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int64, device="cuda")
-        m = mono_export(self.handle, ids, count, seen, resident, w, None, n)
-        owns = resident[:m].nonzero()[:, 0]
-        ids, order = torch.sort(ids[:m][owns])
-        return ids, PackedRows.pack(w[owns[order]], group, scale_dtype or torch.float16)
+        stream.synchronize()       # the table writes on its own stream what torch's may have had in use
+        m = mono_export(self.handle, ids, None, None, resident, None, None, n)
+        ids = ids[:m][resident[:m].bool()]
+        del resident
+        ids = torch.sort(ids).values
+        packed = PackedRows.empty(ids.numel(), self.dim, group, scale_dtype or torch.float16)
+        step = max(1, self.PACK_BYTES // (4 * self.dim))
+        w = torch.empty((min(step, ids.numel()), self.dim), dtype=torch.float32, device="cuda")
+        for lo in range(0, ids.numel(), step):
+            part = ids[lo:lo + step]
+            stream.synchronize()
+            mono_read_rows(self.handle, part, part.numel(), w)
+            mono_pack_rows(w[:part.numel()], packed.q[lo:lo + step], packed.scales[lo:lo + step], group)
+        return ids, packed
 
     def rehash(self, new_key_cells: int = 0, new_seed: int = 0):
         mono_rehash(self.handle, new_key_cells, new_seed)

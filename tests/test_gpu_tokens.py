@@ -283,3 +283,37 @@ def test_rows_are_replaced_in_a_graph():
     graph.replay()
     want = PackedRows.pack(new, 32)
     assert torch.equal(packed.q[[7, 0]], want.q) and torch.equal(packed.scales[[7, 0]], want.scales)
+
+
+@pytest.mark.parametrize("stream", ["its own", "another"])
+def test_an_export_has_no_more_fp32_rows_at_once_than_it_says(stream, monkeypatch):
+    tracked, owners, dim = 1 << 19, 5000, 512
+    table = mb.MonoTable(1 << 16, dim, 2, 0, key_cells=1 << 20, lr=0.1, init_scale=0.5, seed=1)
+    ids = torch.randperm(tracked, device="cuda") + 1
+    bag = torch.zeros(1, dim, device="cuda")
+    for part in (*ids.split(1 << 16), ids[:owners]):           # the first pass counts them, the second gives some a row
+        table.apply_grads(part, torch.tensor([0, part.numel()], device="cuda"), bag, 1)
+    want = table.probe(ids[:owners].sort().values)["w"]
+    monkeypatch.setattr(mb.MonoTable, "PACK_BYTES", 4 * dim * 1024 + 100)      # (1024 rows, five times)
+    torch.cuda.synchronize()
+    other = torch.cuda.current_stream() if stream == "its own" else torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        torch.cuda.empty_cache()
+        if stream == "another":                                 # memory that is free again, but for work that is under way
+            busy = torch.empty(1 << 24, device="cuda")
+            for _ in range(200):
+                busy.fill_(7.0)
+            del busy
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        got, packed = table.export_packed(group=32, scale_dtype=F32)
+    other.synchronize()
+    taken = torch.cuda.max_memory_allocated() - before
+    # the buffer, the packed rows (dim / 2 + 4 * dim / 32 bytes each), and up to ten 64-bit numbers for each ID
+    assert taken < 4 * dim * 1024 + owners * (dim // 2 + dim // 8) + 80 * tracked < 4 * dim * tracked // 16
+    assert torch.equal(got, ids[:owners].sort().values) and len(packed) == owners
+    again = PackedRows.pack(torch.from_numpy(want).cuda(), 32, F32)
+    assert torch.equal(packed.q, again.q) and torch.equal(packed.scales, again.scales)
+    monkeypatch.setattr(mb.MonoTable, "PACK_BYTES", 1)         # a row at a time
+    assert torch.equal(table.export_packed(group=32, scale_dtype=F32)[1].q, again.q)
+    table.close()
