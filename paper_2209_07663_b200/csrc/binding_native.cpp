@@ -276,7 +276,7 @@ PyObject* group_push(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---- operators on plain matrices: tensors as they are, on the current stream of their device ----
 
 // The tensors of one call, in turn.  All of them have to be on one CUDA device; it is the current one while the call
-// runs, and an output's version goes up, so that autograd sees that it was written.
+// runs, and an output's version goes up, so that autograd sees that it was written (unless the call was refused).
 struct Operands {
   const at::Device* device = nullptr;
 
@@ -314,9 +314,11 @@ struct Operands {
     }
     m->data = t->data_ptr();
     m->pad_ = 0;
-    if (written && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+    if (written) writes(*t);
     return true;
   }
+
+  void writes(const at::Tensor& t) { written_[n_written_++] = &t; }
 
   bool tokens(PyObject* x, const void** data, int32_t* type, i64* n) {
     const at::Tensor* t = tensor(x, "tokens");
@@ -362,11 +364,18 @@ struct Operands {
   PyObject* run(C&& call) {
     const c10::DeviceGuard guard(at_);
     const ptr stream = c10::cuda::getCurrentCUDAStream(at_.index()).stream();
-    return without_gil([&] { return call(stream); });
+    int rc = MONO_OK;
+    PyObject* const result = without_gil([&] { return rc = call(stream); });
+    if (rc == MONO_OK || rc == MONO_ERR_CUDA)
+      for (int k = 0; k < n_written_; ++k)
+        if (!written_[k]->is_inference()) written_[k]->unsafeGetTensorImpl()->bump_version();
+    return result;
   }
 
  private:
   at::Device at_ = at::kCPU;
+  const at::Tensor* written_[2] = {};
+  int n_written_ = 0;
 };
 
 bool number(PyObject* x, float* out) {
@@ -424,10 +433,8 @@ PyObject* pack_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   mono_matrix_t rows;
   mono_packed_t packed;
   if (!expects(n, 4) || !o.matrix(a[0], "rows", false, &rows) || !o.packed(a[1], a[2], a[3], rows.cols, &packed)) return nullptr;
-  for (PyObject* x : {a[1], a[2]}) {
-    const at::Tensor& t = THPVariable_Unpack(x);
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
-  }
+  o.writes(THPVariable_Unpack(a[1]));
+  o.writes(THPVariable_Unpack(a[2]));
   return o.run([&](ptr s) { return fn<decltype(&mono_pack_rows)>(F_PACK_ROWS)(&rows, &packed, s); });
 }
 

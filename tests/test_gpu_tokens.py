@@ -317,3 +317,39 @@ def test_an_export_has_no_more_fp32_rows_at_once_than_it_says(stream, monkeypatc
     monkeypatch.setattr(mb.MonoTable, "PACK_BYTES", 1)         # a row at a time
     assert torch.equal(table.export_packed(group=32, scale_dtype=F32)[1].q, again.q)
     table.close()
+
+
+def test_a_refused_call_leaves_an_outputs_version_alone():
+    w, t, o = randn(10, 8), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.empty(4, 8, device="cuda")
+    p = PackedRows.pack(w, 32)
+    refused = [
+        (o, lambda: mb.mono_token_rows(w, t[:3], o)),
+        (o, lambda: mb.mono_token_rows(w, t.cpu(), o)),
+        (w, lambda: mb.mono_token_rows_grad(o, t[:3], w)),
+        (w, lambda: mb.mono_token_rows_grad(o.repeat(200, 1), t.repeat(200), w, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))),
+        (w, lambda: mb.mono_token_rows_grad(o, t, w, workspace=1)),
+        (p.q, lambda: mb.mono_pack_rows(w[:5], p.q, p.scales, 32)),
+        (p.scales, lambda: mb.mono_pack_rows(w[:5], p.q, p.scales, 32)),
+        (o, lambda: mb.mono_packed_token_rows(p.q, p.scales, 32, t[:3], o)),
+        (o, lambda: mb.mono_packed_token_rows(p.q, p.scales, 48, t, o)),
+        (o, lambda: mb.mono_packed_scores(p.q, p.scales, 32, randn(4, 8), o)),
+        (o, lambda: mb.mono_packed_scores(p.q, p.scales, 32, randn(17, 8), o)),
+    ]
+    for written, call in refused:
+        version = written._version
+        with pytest.raises((mb.MonoError, ValueError, TypeError)):
+            call()
+        assert written._version == version
+    x = torch.ones(4, 8, device="cuda", requires_grad=True) * 2
+    y = x.square().sum()
+    with pytest.raises(mb.MonoError):
+        mb.mono_token_rows(w, t[:3], x.detach())
+    y.backward()                                           # (what was not written is not "modified")
+    made = torch.empty(1, 10, device="cuda")
+    for written, call in [(o, lambda: mb.mono_token_rows(w, t, o)), (w, lambda: mb.mono_token_rows_grad(o, t, w)),
+                          (p.q, lambda: mb.mono_pack_rows(w, p.q, p.scales, 32)), (p.scales, lambda: mb.mono_pack_rows(w, p.q, p.scales, 32)),
+                          (o, lambda: mb.mono_packed_token_rows(p.q, p.scales, 32, t, o)),
+                          (made, lambda: mb.mono_packed_scores(p.q, p.scales, 32, randn(1, 8), made))]:
+        version = written._version
+        call()
+        assert written._version == version + 1
