@@ -59,8 +59,7 @@ def build_native(force: bool = False) -> str:
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            *[f"-isystem{d}" for d in cpp_extension.include_paths()], f"-I{sysconfig.get_paths()['include']}",
-           f"-isystem{os.path.join(os.path.dirname(os.path.dirname(find_nvcc())), 'include')}",
-           NATIVE_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
+           NATIVE_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"]
     subprocess.check_call(cmd)
     os.replace(tmp, native)
     return native

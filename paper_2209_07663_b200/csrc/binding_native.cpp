@@ -15,7 +15,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
-#include <c10/cuda/CUDAStream.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/mono.h"
@@ -363,7 +363,9 @@ struct Operands {
   template <typename C>
   PyObject* run(C&& call) {
     const c10::DeviceGuard guard(at_);
-    const ptr stream = c10::cuda::getCurrentCUDAStream(at_.index()).stream();
+    // (through the device's interface: torch's CUDA library and headers need not be there to build this file)
+    const c10::impl::VirtualGuardImpl device(at_.type());
+    const ptr stream = device.getStreamNativeHandle(device.getStream(at_));
     int rc = MONO_OK;
     PyObject* const result = without_gil([&] { return rc = call(stream); });
     if (rc == MONO_OK || rc == MONO_ERR_CUDA)

@@ -192,3 +192,29 @@ def test_another_torch_gets_an_extension_of_its_own(monkeypatch):
     assert made and theirs != mine
     with pytest.raises(RuntimeError, match="missing"):
         mb._load_native(mb.load_library())
+
+
+def test_the_extension_is_built_without_nvcc_and_without_torchs_cuda(monkeypatch, tmp_path):
+    # as in a torch that has no CUDA, beside a library that was built elsewhere
+    from paper_2209_07663_b200 import build
+    from torch.utils import cpp_extension
+    made, run = [], build.subprocess.check_call
+
+    def no_nvcc():
+        raise RuntimeError("nvcc not found")
+
+    def compiler(cmd):
+        made.append(cmd)
+        return run(cmd)
+    monkeypatch.setattr(build, "find_nvcc", no_nvcc)
+    monkeypatch.setattr(build.subprocess, "check_call", compiler)
+    target = str(tmp_path / "extension.so")
+    monkeypatch.setattr(build, "native_path", lambda: target)
+    assert build.build_native(force=True) == target and os.path.exists(target)
+    assert not [x for x in made[0] if x.startswith("-l") and "cuda" in x]
+    headers = [x[len("-isystem"):] for x in made[0] if x.startswith("-isystem")]
+    assert headers == cpp_extension.include_paths()
+    seen = subprocess.run([made[0][0], "-std=c++17", "-M", *[x for x in made[0] if x.startswith(("-I", "-D", "-isystem"))], build.NATIVE_SOURCE],
+                          capture_output=True, text=True, timeout=600)
+    assert seen.returncode == 0, seen.stderr[-2000:]
+    assert not [x for x in seen.stdout.split() if "/cuda" in x]
