@@ -49,8 +49,17 @@ def token_rows(weight, tokens, scale: float = 1.0, padding: int = -1, dtype=None
     return _TokenRows.apply(weight, tokens.contiguous(), float(scale), int(padding), dtype)
 
 
+def _no_gradient(call, **tensors):
+    if torch.is_grad_enabled():
+        for name, x in tensors.items():
+            if x is not None and x.requires_grad:
+                raise RuntimeError(f"{call} has no gradient, but {name} requires one: detach it, or call under torch.no_grad()")
+
+
 class PackedRows:
     """Rows in 4 bits a column with one scale per group of columns: value = (q - 8) * scale.
+
+    For serving: nothing here has a gradient, and `rows` and `scores` refuse tensors that would need one.
 
     `q` is uint8 [rows, bytes], two columns in a byte (the even one in the low half), a row's bytes rounded up to a multiple
     of 16; `scales` is [rows, groups].  Both are plain tensors: a program saves, loads and moves them as it likes.
@@ -100,6 +109,7 @@ class PackedRows:
 
     def rows(self, tokens, scale: float = 1.0, padding: int = -1, dtype=torch.float32, out=None):
         """scale * the rows that `tokens` name; zeros where a token is `padding` or names none."""
+        _no_gradient("rows", out=out, scales=self.scales)
         tokens = tokens.contiguous()
         if out is None:
             out = torch.empty((*tokens.shape, self.cols), dtype=dtype, device=self.q.device)
@@ -110,6 +120,7 @@ class PackedRows:
 
     def scores(self, x, dtype=torch.float32, out=None):
         """<x, row> for every row: [rows] of one vector, [vectors, rows] of up to binding.MONO_MAX_SCORED."""
+        _no_gradient("scores", x=x, out=out, scales=self.scales)
         if x.shape[-1] != self.cols:
             raise ValueError(f"x: {self.cols} columns are expected")
         if out is None:

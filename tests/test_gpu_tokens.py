@@ -353,3 +353,22 @@ def test_a_refused_call_leaves_an_outputs_version_alone():
         version = written._version
         call()
         assert written._version == version + 1
+
+
+def test_packed_rows_refuse_what_would_need_a_gradient():
+    p, t = PackedRows.pack(randn(10, 8).requires_grad_(), 32), torch.arange(3, device="cuda")      # (packing is of the values)
+    x, leaf, made = randn(2, 8).requires_grad_(), torch.zeros(3, 8, device="cuda", requires_grad=True), torch.zeros(2, 10, device="cuda").requires_grad_()
+    learned = PackedRows(p.q, p.scales.float().requires_grad_(), 8, 32)
+    calls = [lambda: p.scores(x), lambda: p.scores(x * 2), lambda: p.scores(x.detach(), out=made), lambda: p.rows(t, out=leaf), lambda: p.rows(t, out=leaf * 2),
+             lambda: learned.rows(t), lambda: learned.scores(x.detach())]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="no gradient"):
+            call()
+    assert bool((leaf == 0).all()) and bool((made == 0).all())
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            assert torch.equal(p.scores(x), p.scores(x.detach()))
+            assert torch.equal(learned.scores(x), p.scores(x))
+            p.rows(t, out=leaf.detach())
+    assert torch.equal(leaf.detach(), p.rows(t))
+    assert p.scores(x.detach()).shape == (2, 10)
