@@ -306,7 +306,8 @@ struct Operands {
       m->rows = t->size(0);
       m->stride = m->rows > 1 ? t->stride(0) : m->cols;
     } else if (t->is_contiguous()) {
-      m->rows = m->cols ? t->numel() / m->cols : 0;
+      m->rows = 1;                                         // (a single row even where it has no columns: scores of no packed rows)
+      for (i64 d = 0; d + 1 < dims; ++d) m->rows *= t->size(d);
       m->stride = m->cols;
     } else {
       PyErr_Format(PyExc_ValueError, "%s: the columns of a row have to be next to each other", name);

@@ -372,3 +372,16 @@ def test_packed_rows_refuse_what_would_need_a_gradient():
             p.rows(t, out=leaf.detach())
     assert torch.equal(leaf.detach(), p.rows(t))
     assert p.scores(x.detach()).shape == (2, 10)
+
+
+def test_scores_of_no_packed_rows():
+    p = PackedRows.pack(randn(5, 16)[:0], 32)
+    for shape in ((16,), (1, 16), (3, 16), (2, 3, 16), (0, 16), (2, 0, 16), (1, 1, 16)):
+        assert p.scores(randn(*shape)).shape == (*shape[:-1], 0)
+    mb.mono_packed_scores(p.q, p.scales, 32, randn(16), torch.empty(0, device="cuda"))
+    for x, out in ((randn(2, 16), torch.empty(0, device="cuda")), (randn(16), torch.empty(2, 0, device="cuda"))):
+        with pytest.raises(mb.MonoError):
+            mb.mono_packed_scores(p.q, p.scales, 32, x, out)
+    # where rows are looked up, they have columns
+    with pytest.raises(mb.MonoError):
+        mb.mono_token_rows(randn(4, 0), torch.zeros(1, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda"))
