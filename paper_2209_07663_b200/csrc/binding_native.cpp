@@ -286,6 +286,7 @@ struct Operands {
     if (!t.is_cuda()) { PyErr_Format(PyExc_ValueError, "%s is not on a CUDA device (there is no CPU path)", name); return nullptr; }
     if (!device) { at_ = t.device(); device = &at_; }
     if (t.device() != at_) { PyErr_Format(PyExc_ValueError, "%s is on another device than the tensors before it", name); return nullptr; }
+    if (t.is_neg()) { PyErr_Format(PyExc_ValueError, "%s is a view that negates what its memory holds: resolve_neg() it", name); return nullptr; }
     return &t;
   }
 

@@ -29,7 +29,7 @@ class _TokenRows(torch.autograd.Function):
     def backward(ctx, grad_out):
         tokens, = ctx.saved_tensors
         cols = grad_out.shape[-1]
-        grad_out = grad_out.reshape(-1, cols)             # (a view, or a copy where the rows do not lie in one)
+        grad_out = grad_out.resolve_neg().reshape(-1, cols)      # (a view, or a copy where the rows do not lie in one)
         if cols > 1 and grad_out.stride(1) != 1:
             grad_out = grad_out.contiguous()              # as a sum's gradient, which is one number everywhere
         grad_weight = torch.empty((ctx.vocabulary, cols), dtype=ctx.grad_dtype, device=grad_out.device)

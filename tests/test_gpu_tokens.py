@@ -385,3 +385,29 @@ def test_scores_of_no_packed_rows():
     # where rows are looked up, they have columns
     with pytest.raises(mb.MonoError):
         mb.mono_token_rows(randn(4, 0), torch.zeros(1, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda"))
+
+
+def test_views_that_negate_their_memory_are_refused():
+    w = torch.complex(randn(5, 1), randn(5, 1, seed=2)).conj().imag        # (one column: its rows are two elements apart)
+    assert w.is_neg()
+    t, out = torch.arange(3, device="cuda"), torch.empty(3, 1, device="cuda")
+    packed = PackedRows.pack(randn(3, 1), 32)
+    for call in (lambda: mb.mono_token_rows(w, t, out), lambda: mb.mono_token_rows_grad(out, t, w), lambda: mb.mono_token_rows(out, t, w[:3]),
+                 lambda: PackedRows.pack(w), lambda: packed.scores(w)):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            call()
+    mb.mono_token_rows(w.resolve_neg(), t, out)
+    assert torch.equal(out, w[:3].clone())
+
+
+@pytest.mark.parametrize("cols", [1, 6])
+def test_gradients_that_are_such_views(cols):
+    weight, tokens, other = randn(9, cols).requires_grad_(), torch.arange(20, device="cuda") % 9, randn(20, cols, seed=1)
+    pick = randn(20, cols, seed=2)
+    rows = token_rows(weight, tokens)
+    seen = []
+    rows.register_hook(lambda g: seen.append(g.is_neg()))
+    z = torch.complex(other, pick)
+    rows.backward(z.conj().imag)
+    assert seen == [True]
+    check_grad(weight.grad, None, -pick, tokens, 1.0, -1)
