@@ -84,32 +84,29 @@ __device__ __forceinline__ Vec<T, N> from_floats(const float (&f)[N]) {
   return x;
 }
 
-// 8 elements from any address: the aligned 16-byte words that hold them, moved by as many bytes as the first one begins behind
-// a multiple of 16.  All of the words have to be readable.
+// 8 elements of 16 bits from any address: the two aligned 16-byte words that hold them, moved by as many bytes as the first one begins
+// behind a multiple of 16.  Both words have to be readable.
 template <typename T>
-__device__ __forceinline__ void load_shifted(const T* from, uint32_t (&w)[2 * sizeof(T) + 4]) {
+__device__ __forceinline__ void load_shifted(const T* from, uint32_t (&w)[8]) {
+  static_assert(sizeof(T) == 2, "");
   const uint4* const at = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
-  constexpr int N = sizeof(T) / 2 + 1;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
+  for (int k = 0; k < 2; ++k) {
     const uint4 x = at[k];
     w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
   }
 }
 template <typename T>
-__device__ __forceinline__ Vec<T, 8> shifted(const uint32_t (&in)[2 * sizeof(T) + 4], uint32_t bytes) {
-  constexpr int N = 2 * sizeof(T);                         // words of the 8 elements
-  uint32_t w[N + 4];
+__device__ __forceinline__ Vec<T, 8> shifted(const uint32_t (&in)[8], uint32_t bytes) {
+  uint32_t w[8];
 #pragma unroll
-  for (int k = 0; k < N + 4; ++k) w[k] = in[k];
+  for (int k = 0; k < 8; ++k) w[k] = in[k];
 #pragma unroll
-  for (int k = 0; k < N + 2; ++k) w[k] = bytes & 8 ? w[k + 2] : w[k];
+  for (int k = 0; k < 6; ++k) w[k] = bytes & 8 ? w[k + 2] : w[k];
 #pragma unroll
-  for (int k = 0; k < N + 1; ++k) w[k] = bytes & 4 ? w[k + 1] : w[k];
-  if (sizeof(T) == 2) {
+  for (int k = 0; k < 5; ++k) w[k] = bytes & 4 ? w[k + 1] : w[k];
 #pragma unroll
-    for (int k = 0; k < N; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (bytes & 2) * 8);
-  }
+  for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (bytes & 2) * 8);
   Vec<T, 8> x;
   memcpy(&x, w, sizeof(x));
   return x;
@@ -232,34 +229,21 @@ int with_width(int v, F&& f) {
 
 // Launch of a kernel that waits for the stream's previous kernel itself (after_previous_kernel), so that its
 // launch is prepared while that one runs.
-struct Launch {
-  dim3 grid;
-  unsigned block;
-  size_t shared;
-  cudaStream_t stream;
-  unsigned cluster;        // blocks along x, 0: none
-};
 template <typename... P, typename... A>
-inline int launch_operator(const Launch& l, void (*kernel)(P...), A&&... args) {
+inline int launch_operator(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, cudaStream_t s, A&&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = l.grid;
-  cfg.blockDim = dim3(l.block, 1, 1);
-  cfg.dynamicSmemBytes = l.shared;
-  cfg.stream = l.stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {l.cluster, 1, 1};
-  cfg.attrs = attr;
-  cfg.numAttrs = l.cluster ? 2 : 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block, 1, 1);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
   if (cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...) == cudaSuccess) return MONO_OK;
   cudaGetLastError();                                       // (reported here, not by the next call that asks)
   return MONO_ERR_CUDA;
-}
-template <typename... P, typename... A>
-inline int launch_operator(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, cudaStream_t s, A&&... args) {
-  return launch_operator(Launch{grid, block, shared, s, 0u}, kernel, std::forward<A>(args)...);
 }
 
 }  // namespace mono

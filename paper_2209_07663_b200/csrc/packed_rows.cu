@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) packed_scores_kernel(Packe
         // of_group: the operands' powers of two and the weights' 2^-10, taken back
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-          const float f = U == 1 ? to_float(own[j][0]) : __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4));
+          const float f = __shfl_sync(0xFFFFFFFFu, to_float(own[j][u / 4]), (lane & ~3) | (u % 4));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             total[j / 2][nt][j % 2 * 2] += f * (of_group[nt].x * sum[j / 2][nt][j % 2 * 2]);

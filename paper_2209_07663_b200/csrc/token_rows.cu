@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* w
   const W* const end = weight + (tokens.vocab - 1) * weight_stride + cols;
   uint32_t t[ROWS];
   tokens.rows(row0, groups, t);
-  uint32_t in[kMoves][2 * sizeof(W) + 4];
+  uint32_t in[kMoves][8];
 #pragma unroll
   for (int k = 0; k < kMoves; ++k) {
     const uint32_t row = t[k / PIECES];
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* w
     if (row == kNoToken || c >= cols) continue;
     const W* const from = weight + row * weight_stride + c;
     // (the aligned words reach up to 15 bytes beyond the 8 elements, and those up to 7 elements beyond the row)
-    if (from - 16 / sizeof(W) >= begin && from + 8 + 16 / sizeof(W) <= end) {
+    if (from - 8 >= begin && from + 16 <= end) {
       load_shifted(from, in[k]);
     } else {
       W x[8];
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads) token_rows_shifted_kernel(const W* w
     float f[8] = {};
     if (row != kNoToken) {
       const W* const from = weight + row * weight_stride + c;
-      const bool whole = from - 16 / sizeof(W) >= begin && from + 8 + 16 / sizeof(W) <= end;
+      const bool whole = from - 8 >= begin && from + 16 <= end;
       to_floats(shifted<W>(in[k], whole ? (uint32_t)reinterpret_cast<uintptr_t>(from) & 15 : 0), f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] *= scale;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) rank_tokens_kernel(TokenList tokens,
 
 // (marks: cleared, by the blocks that would fill zeros, where this is the first pass)
 template <int KEYS>
-__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, int64_t n, int shift, int bits, uint32_t* __restrict__ counts, uint4* marks, int64_t mark_words,
+__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(Keys keys, int shift, int bits, uint32_t* __restrict__ counts, uint4* marks, int64_t mark_words,
                                                                     Zeros zeros) {
   after_previous_kernel();
   release_next_kernel();
@@ -846,7 +846,7 @@ int launch_grad(const mono_matrix_t& grad, const TokenList& tokens, float scale,
       if (marked) { z.first = (unsigned)p.tiles; grid = dim3((unsigned)p.tiles + 16); }
       const auto with_keys = [&](auto f) { return with_width(p.keys, f); };
       rc = with_keys([&](auto k) {
-        return launch_operator(count_digits_kernel<decltype(k)::value>, grid, kSortThreads, 0, s, keys, n, shift, p.bits, w.counts, reinterpret_cast<uint4*>(marked),
+        return launch_operator(count_digits_kernel<decltype(k)::value>, grid, kSortThreads, 0, s, keys, shift, p.bits, w.counts, reinterpret_cast<uint4*>(marked),
                                (vocab + 15) / 16, z);
       });
       if (rc != MONO_OK) return rc;
