@@ -367,3 +367,49 @@ def test_calls_at_once_on_two_streams():
     torch.cuda.synchronize()
     for k in range(2):
         check_grad(gots[k], None, grads[k], tokens[k], 1.0, -1)
+
+
+# ---- sums by their depth, and what no list of marks is kept for ----
+
+def depth_of(n, cols, count):
+    """The most additions on the way of a term to its row's sum, for the rows that `count` tokens name.  Up to 512 tokens: a group's run of
+    ceil(512 / groups) positions, then the pieces of the block's groups.  Beyond: a run of 8 to 64 positions, then a block's pieces (two a group at most),
+    then one of each block that has the row's terms.  A group has a thread for each 8 columns, up to 32 (a power of two), a block 256 threads."""
+    lanes = 1
+    while lanes < 32 and lanes * 8 < -(-cols // -(-cols // 256)):
+        lanes *= 2
+    groups = 256 // lanes
+    if n <= 512:
+        return torch.clamp(count, max=-(-512 // groups) + 2 * groups)
+    return torch.minimum(count, 64 + 2 * groups + 2 + count // (8 * groups))
+
+
+@pytest.mark.parametrize("n,vocab", [(300, 2), (512, 1), (2049, 3), (8193, 3), (60000, 2)])
+@pytest.mark.parametrize("cols", [1, 4, 8, 24, 100, 256, 515, 1024])
+def test_gradient_of_rows_with_many_terms(n, vocab, cols):
+    grad = randn(n, cols, dtype=BF16).abs()                # (of one sign, so that errors add up as far as they go)
+    tokens = some_tokens(n, vocab, strange=False)
+    got = torch.empty((vocab, cols), device="cuda")
+    mb.mono_token_rows_grad(grad, tokens, got)
+    total, size, count = grad64(grad, tokens, vocab, 1.0, -1)
+    # each addition is off by 2^-24 of a sum of at most `size` (2^-23 covers the second order), and the product and the output as in check_grad
+    tol = size * (depth_of(n, cols, count)[:, None].double() + 2) * 2.0 ** -23
+    assert bool(((got.double() - total).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("n", [8193, 50000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_a_vocabulary_too_large_for_marks(n, accumulate):
+    vocab, cols = (1 << 24) + 77, 3
+    grad, tokens = randn(n, cols, dtype=BF16), some_tokens(n, vocab)
+    tokens[:n // 3] = tokens[:n // 3] % 50 * (vocab // 50) + 1       # (some rows with many terms)
+    tokens[5], tokens[6] = 0, vocab - 1
+    before = torch.full((vocab, cols), 0.5, dtype=F16, device="cuda")
+    got = before.clone()
+    mb.mono_token_rows_grad(grad, tokens, got, scale=0.5, accumulate=accumulate)
+    there = (tokens >= 0) & (tokens < vocab)
+    rows, place = torch.unique(tokens[there], return_inverse=True)
+    # the rows that tokens name, as a small vocabulary of their own, and all the others
+    check_grad(got[rows], before[rows] if accumulate else None, grad[there], place, 0.5, -1)
+    got[rows] = 0.5 if accumulate else 0.0
+    assert bool((got == (0.5 if accumulate else 0.0)).all())
