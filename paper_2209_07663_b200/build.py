@@ -13,7 +13,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 HEADER = os.path.join(PKG, "..", "include", "mono.h")
 LIB = os.path.join(PKG, "libmono.so")
-# the same sources with -DMONO_DEBUG: every index the library computes for itself is range-checked
+# the same sources with -DMONO_DEBUG: every index a table's kernels compute for themselves is range-checked
 # on the device and a bad one reported through the status bits (binding: MONO_LIBRARY=checked)
 LIB_CHECKED = os.path.join(PKG, "libmono_checked.so")
 # the hot calls' Python side; touches no table and needs no nvcc

@@ -32,8 +32,9 @@ inline PackedView view(const mono_packed_t& p) {
 
 // ---------------------------------------------------------------------------
 // Packing: 8 threads a group of columns, group / 8 neighbouring columns each, so that every thread writes whole bytes.  A block has the groups of
-// blockIdx.y's share of kPackGroups / block_groups rows.  (131072 rows of 1024 fp32 columns: 172 us, of which the bytes are 93; what a thread does once for its columns
-// is the rest.  With half as many columns each, single columns read and a 64-bit division to find them it took 288.)
+// blockIdx.y's share of kPackGroups / block_groups rows.  (131072 rows of 1024 columns: 171 us in fp32, 185 in bf16, where the bytes are 93 and 52: what bounds it is
+// what a thread does for each column, rounding and the choice to divide.  With half as many columns a thread, single columns read and a 64-bit division to find them
+// fp32 rows took 288.)
 // ---------------------------------------------------------------------------
 constexpr int kPackThreads = 8, kPackGroups = kThreads / kPackThreads;
 
@@ -93,7 +94,9 @@ __global__ void __launch_bounds__(kThreads) pack_rows_kernel(const W* rows, int6
 
 // ---------------------------------------------------------------------------
 // Rows by token of packed rows.  A thread makes the 8 columns of a 32-bit word, and keeps four words and their scales in flight behind the read
-// of its tokens: four of one row where rows are wide, one of each of four rows where `lanes` threads cover a row.
+// of its tokens: four of one row where rows are wide, one of each of four rows where `lanes` threads cover a row.  (262144 tokens of 128 columns, bf16 out: 19.5 us, of
+// which the bytes are 11; issue slots are 82 % used.  Where 8 does not divide the columns, a column takes two shuffles and a store: 65536 tokens of
+// 130 columns 18 us, of 128 columns 6.)
 // ---------------------------------------------------------------------------
 constexpr int kMoves = 4;
 
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // ---------------------------------------------------------------------------
 // Scores.  out[m, v] = sum over groups g of s[v, g] * (sum over c in g of x[m, c] * (q[v, c] - 8)).
 //
-// The bytes of q bound it (half a byte for 2 * m operations), if a weight becomes an operand in few enough instructions: the tensor
+// The bytes of q would bound it (half a byte for 2 * m operations) if a weight became an operand in few enough instructions: the tensor
 // cores' 16-bit products take 16 rows and 8 vectors at once.  As the bits of an fp16, 4 bits in the lowest places are q * 2^-24 and in
 // the next ones 16 * q * 2^-24, subnormal and exact; times 2^14 or 2^10, less 8 * 2^-10, they are (q - 8) * 2^-10: an AND and
 // a multiply-add for two weights, and a shift for each eight.  (Left subnormal, with the 8 taken off the sums, they took 71 us instead of
@@ -173,8 +176,11 @@ __global__ void __launch_bounds__(kThreads) packed_token_rows_kernel(PackedView 
 // pieces: 8 vectors against 131072 rows of 4096 columns took 84 us when they took 80 this way; 128 columns a move 75, 256 now 73.)  Where there
 // are few rows, `split` warps share 32 rows, a run of columns each.  Scales are read ahead by the four threads of a row, one each.
 //
-// Measured: 73 us for those, 3.8 TB/s; one vector against 50001 rows of 1024 columns 8.9 us.  Issue slots are 59 % and the ALU pipe 47 % used: what bounds them
-// is making operands, not bytes.
+// Measured: 73 us for those, 3.8 TB/s; one vector against them 58, against 50001 rows of 1024 columns 8.9, against a million of 128 columns 31 (a stage is
+// 32 rows, however short they are: 2.3 TB/s).  Nothing is used up (for 8 vectors issue slots 60 %, ALU pipe 47 %, tensor cores 25 %, HBM 58 %): with three warps a scheduler, which
+// is what the vectors' operands in shared memory leave room for, it is the way from the stage through operands and products to the sums, one after the other, and
+// reading the vectors' operands, as many bytes from shared memory as the weights.  For 16 vectors, or rows of more than 4096 columns, there are fewer warps still
+// (16 against 50000 rows of 2048 columns: 37 us, of which the bytes are 8.6).
 // ---------------------------------------------------------------------------
 constexpr int kTileRows = 32;
 constexpr int kBlockColumns = 256, kBlockBytes = kBlockColumns / 2;

@@ -119,7 +119,7 @@ struct __align__(8) CallState {
   unsigned int bad_offsets;              // this call's offsets were malformed: occurrences are checked one by one
 };
 
-// Checked build (-DMONO_DEBUG): every index the library computes for itself -- a segment
+// Checked build (-DMONO_DEBUG): every index a table's kernels compute for themselves -- a segment
 // position, a place in one of the per-call lists, a slot of the per-call set, a position of
 // the free-row stack -- is tested against the size of its array before it is used; one that
 // falls outside sets the sticky MONO_DEV_INTERNAL bit and the access is skipped.  The release

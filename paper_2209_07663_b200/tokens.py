@@ -3,7 +3,8 @@
 A feature whose vocabulary is fixed needs no hash table: its rows are a matrix and a token is a row's number.
 `token_rows` is the input layer of a sequence model beside the tables' pooled features; `PackedRows` is what of a
 matrix, or of a trained table's rows, goes to a serving process: looked up again, or scored against a few vectors.
-Everything runs in the CUDA library (include/mono.h); there is no CPU path.
+Everything runs in the CUDA library (include/mono.h); there is no CPU path.  What records torch operations while they run (torch.jit.trace, make_fx)
+does not see the library's: it would record the empty outputs alone.
 """
 from __future__ import annotations
 
@@ -81,7 +82,9 @@ class PackedRows:
 
     @classmethod
     def pack(cls, rows, group: int = 64, scale_dtype=torch.float16):
-        """Of a matrix on the device (each column within half a scale of what it was)."""
+        """Of a matrix on the device.  Each column is within half a scale of what it was, a scale being a seventh of the largest
+        column of its group, where scale_dtype has room for it: float16 does not for groups whose largest column is beyond 4.5e5 (NaN) or
+        below 3e-6 (off by more; zeros below 2e-7), bfloat16 and float32 do."""
         p = cls.empty(rows.shape[0], rows.shape[1], group, scale_dtype, rows.device)
         mb.mono_pack_rows(rows, p.q, p.scales, group)
         return p
