@@ -565,8 +565,8 @@ int mono_token_rows(const mono_matrix_t* weight, const void* tokens, int32_t tok
  *  accumulate 0: grad_weight[v, :] = G[v, :] for every row v, zeros where no token is v;
  *  accumulate 1: grad_weight[v, :] += G[v, :] for the rows that a token names (the sum rounded once), the other
  *                rows are neither read nor written.
- * The tokens are sorted (stably), and a row's terms are added up in an order that depends on the tokens alone: the same call on
- * the same inputs gives the same bits.  (mono_apply_grads makes no such promise.)
+ * The tokens are sorted (stably), and a row's terms are added up in an order that depends on the tokens and the number of columns
+ * alone: the same call on the same values gives the same bits, wherever the matrices lie.  (mono_apply_grads makes no such promise.)
  *  grad_out     [n_tokens, cols]
  *  grad_weight  [vocabulary, cols], any of the types
  *  workspace    DEVICE, 256-byte aligned, workspace_bytes of it: at least what mono_token_rows_grad_workspace says for

@@ -141,7 +141,8 @@ int launch_token_rows(const mono_matrix_t& weight, const TokenList& tokens, floa
 // consecutive.  A group of up to 32 threads adds up a run of sorted positions in order and writes the rows that begin and end in
 // it; what it has of other rows, a piece in front and a piece at the end, a block joins over its groups' runs in
 // shared memory, and join_rows_kernel over the blocks, both in the order of the positions.  The terms are read once and
-// no order depends on timing, so the result has the same bits every time.
+// no order depends on timing or on where the matrices lie, so the result has the same bits every time.  (The sum of what is there and the
+// product is written as one operation: left to the compiler, some widths of the moves rounded the product and others did not.)
 //
 // Three ways to sort, by the number of tokens:
 //   up to kSmallTokens   every block of the summing kernel ranks all tokens in shared memory: no launch of its own
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) =
               for (int r = 0; r < R; ++r) {
                 float f[VEC];
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) f[c] = ADD ? to_float(old[ADD ? u : 0][r].v[c]) + out.scale * sum[r][c] : out.scale * sum[r][c];
+                for (int c = 0; c < VEC; ++c) f[c] = ADD ? fmaf(out.scale, sum[r][c], to_float(old[ADD ? u : 0][r].v[c])) : out.scale * sum[r][c];
                 if (mine[r]) *reinterpret_cast<Vec<O, VEC>*>(at + r * lanes * VEC) = from_floats<O>(f);
               }
             } else {
@@ -665,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, VEC >= 4 || (VEC == 1 && sizeof(G) =
         if (x[k].x == x[k + 1].x) continue;
         if (x[k].x == before_row) out.partial[(int64_t)blockIdx.x * 2 * out.cols + column] = sum;
         else if (x[k].x == behind_row) out.partial[((int64_t)blockIdx.x * 2 + 1) * out.cols + column] = sum;
-        else out.data[x[k].x * out.stride + column] = from_float<O>(ADD ? old[k] + out.scale * sum : out.scale * sum);
+        else out.data[x[k].x * out.stride + column] = from_float<O>(ADD ? fmaf(out.scale, sum, old[k]) : out.scale * sum);
         sum = 0.0f;
       }
     }
@@ -706,7 +707,7 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const Entry* sorted
     }
   }
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) o.v[v] = from_float<O>(add ? to_float(o.v[v]) + out.scale * sum.v[v] : out.scale * sum.v[v]);
+  for (int v = 0; v < VEC; ++v) o.v[v] = from_float<O>(add ? fmaf(out.scale, sum.v[v], to_float(o.v[v])) : out.scale * sum.v[v]);
   *to = o;
 }
 

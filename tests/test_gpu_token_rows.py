@@ -413,3 +413,24 @@ def test_gradient_of_a_vocabulary_too_large_for_marks(n, accumulate):
     check_grad(got[rows], before[rows] if accumulate else None, grad[there], place, 0.5, -1)
     got[rows] = 0.5 if accumulate else 0.0
     assert bool((got == (0.5 if accumulate else 0.0)).all())
+
+
+@pytest.mark.parametrize("n,vocab,cols", [(300, 7, 64), (785, 1, 1024), (1966, 32, 64), (2716, 6, 16), (2910, 5, 2048), (12921, 29, 8), (9000, 400, 264)])
+@pytest.mark.parametrize("g,o", [(F32, F32), (BF16, F32), (F16, BF16)])
+def test_gradient_has_the_same_bits_wherever_its_matrices_lie(n, vocab, cols, g, o):
+    grad, tokens = randn(n, cols, dtype=g, seed=1), some_tokens(n, vocab, seed=2)
+
+    def at(rows, dtype, start, stride):
+        return torch.full((start + rows * stride + 8,), 3.0, dtype=dtype, device="cuda")[start:].as_strided((rows, cols), (stride, 1))
+
+    for accumulate in (False, True):
+        outs = []
+        for k in (0, 1, 2, 4):
+            terms, got = at(n, g, k, cols + k), at(vocab, o, 0, cols)
+            terms.copy_(grad)
+            mb.mono_token_rows_grad(terms, tokens, got, scale=-0.37, padding=0, accumulate=accumulate)
+            far = at(vocab, o, k, cols + k)
+            mb.mono_token_rows_grad(grad, tokens, far, scale=-0.37, padding=0, accumulate=accumulate)
+            outs += [got.contiguous(), far.contiguous()]
+        check_grad(outs[0], torch.full_like(outs[0], 3.0) if accumulate else None, grad, tokens, float(torch.tensor(-0.37)), 0)
+        assert all(torch.equal(outs[0], x) for x in outs[1:])
